@@ -57,7 +57,7 @@ typedef enum {
 
 typedef enum { FLAT_MASK_NONE = 0, FLAT_MASK_CAUSAL = 1 } flat_mask_kind;
 
-typedef enum { FLAT_DTYPE_BF16 = 0 } flat_dtype;
+typedef enum { FLAT_DTYPE_BF16 = 0, FLAT_DTYPE_F32 = 1 /* flat_attn_rope only */ } flat_dtype;
 
 /*
  * Fused attention forward, bf16 in / bf16 out, fp32 accumulation (sections 4-5: fused
@@ -216,6 +216,117 @@ int flat_attn_tile_shape_occupancy(int d, int index);
 int flat_attn_tile_shape_default(int B, int H, int Nq, int d, int mask_kind);
 int flat_attn_fwd_tile(const void* Q, const void* K, const void* V, void* O,
                        int B, int H, int N, int d, float scale, int mask_kind, int tile_shape, void* stream);
+
+/*
+ * Rotary positions of Q and K, in one launch.  Channels a and b of pair i (0 <= i < rot_d / 2) of a row at position p become
+ *     y_a = magnitude * (x_a cos t - x_b sin t),   y_b = magnitude * (x_a sin t + x_b cos t),   t = p * freqs[i];
+ * the channels from rot_d on are copied.  transpose != 0 turns by -t instead: that is the gradient (the rotation is linear, and its
+ * transpose takes the gradient of Y to that of X, magnitude included).
+ *   Q, Q_out: device, [B,Hq,N,d]; K, K_out: device, [B,Hk,N,d], or both NULL (Hk is then ignored).  An output is its own input (in place) or overlaps no
+ *     other buffer (FLAT_ERR_ALIAS).  dtype FLAT_DTYPE_BF16 or FLAT_DTYPE_F32; products and sums in fp32, rounded once.
+ *   d: 32, 64, 96, 128 or 256; rot_d: even, 2 .. d.  layout: FLAT_ROPE_HALF pairs (i, i + rot_d / 2), FLAT_ROPE_INTERLEAVED (2 i, 2 i + 1).
+ *   freqs: device, const double[rot_d / 2], radians per position (8-byte aligned); angles are taken to a turn in 64 bits, so far positions lose nothing.
+ *   positions: device, const int[B,N], any values, or NULL: row n of every batch entry is at position n.
+ */
+enum { FLAT_ROPE_HALF = 0, FLAT_ROPE_INTERLEAVED = 1 };
+int flat_attn_rope(const void* Q, void* Q_out, int Hq, const void* K, void* K_out, int Hk, int B, int N, int d, int dtype, int rot_d,
+                   int layout, const double* freqs, const int* positions, float magnitude, int transpose, void* stream);
+
+/*
+ * Frequencies for flat_attn_rope, written to out[rot_d / 2] (HOST pointer; no GPU is involved): base^(-2 i / rot_d), scaled for contexts
+ * `factor` times longer than the original_len positions that a model was trained on:
+ *   FLAT_ROPE_SCALE_NONE    as they are (factor, original_len, low and high are ignored)
+ *   FLAT_ROPE_SCALE_LINEAR  all divided by factor (positions interpolated)
+ *   FLAT_ROPE_SCALE_BASE    base * factor^(rot_d / (rot_d - 2)) for base: the slowest pair is slowed by factor, the fastest stays (rot_d = 2: as they are)
+ *   FLAT_ROPE_SCALE_BANDS   pairs that turn `high` times or more over original_len stay, those that turn `low` times or fewer are divided by
+ *                           factor, and between the two the share that stays rises linearly with the number of turns
+ * FLAT_ERR_UNSUPPORTED: rot_d not even or not in 2 .. 256, an unknown scaling, or base <= 1, factor < 1, original_len <= 0, or not 0 <= low < high where they count.
+ */
+enum { FLAT_ROPE_SCALE_NONE = 0, FLAT_ROPE_SCALE_LINEAR = 1, FLAT_ROPE_SCALE_BASE = 2, FLAT_ROPE_SCALE_BANDS = 3 };
+int flat_attn_rope_freqs(double* out, int rot_d, double base, int scaling, double factor, double original_len, double low, double high);
+
+/*
+ * A paged cache of keys and values in 8 bits.  It is a pool of n_pages pages; a page holds page_tokens tokens of n_heads heads, and
+ * a request's tokens are found through its row of a page table: token t of batch entry b lies in page page_table[b * max_pages + t / page_tokens].
+ * An id outside [0, n_pages) is a hole: its tokens count for no query, and what is written to them is dropped.  A block of
+ * FLAT_CACHE8_BLOCK tokens of a head has a scale for its keys and one for its values, and a value is code * scale.
+ *   k, v: device, 16-byte aligned, n_pages * n_heads * page_tokens * d codes each.  In memory order, K is [n_pages][n_heads][page_tokens / 16][d / 16]
+ *     [16 tokens][16 channels], V [n_pages][n_heads][page_tokens / 16][d][16 tokens].
+ *   k_scale, v_scale: device, 4-byte aligned, float [n_pages][n_heads][page_tokens / 16], each >= 0 and finite (or NaN: the block is not a number).
+ *   page_tokens: a multiple of 16, at most 65536.  d: 32, 64, 96, 128 or 256.
+ *   format: FLAT_CACHE8_E4M3 (4 exponent and 3 fraction bits, largest 448, no infinity; NaN codes are not to be stored) or FLAT_CACHE8_INT8 (-127 .. 127).
+ *   n_pages * n_heads * page_tokens / 16 is at most 2^31 - 1.
+ * The struct is read during a call and not kept.  Checks common to the entry points that take one: FLAT_ERR_NULL, FLAT_ERR_SHAPE (a count not
+ * positive, page_tokens no multiple of 16, too many blocks), FLAT_ERR_UNSUPPORTED (d, format), FLAT_ERR_ALIGN, FLAT_ERR_ALIAS (outputs overlap).
+ * Lengths, page tables and lists live on the device and are not validated by the host: lengths are clamped to what the page table has room for, ids
+ * are looked at before use, and no value of them makes an access stray.
+ */
+#define FLAT_CACHE8_BLOCK 16
+enum { FLAT_CACHE8_E4M3 = 0, FLAT_CACHE8_INT8 = 1 };
+typedef struct {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    int n_pages, n_heads, page_tokens, d, format;
+} flat_cache8;
+
+/*
+ * New tokens into the cache: row n of batch entry b becomes token lens[b] + n, for n < n_new[b].
+ *   K, V: device, const bf16 [B,n_heads,N,d], 16-byte aligned.  page_table: device, const int [B,max_pages].  lens: device, const int [B], tokens
+ *     of each entry before the call (0 .. max_pages * page_tokens).  n_new: device, const int [B], clamped to [0, N], or NULL: N for every entry.
+ *   Tokens beyond the last page of the table are dropped.  lens is not changed: the caller adds n_new to it.
+ * A block's scale becomes the larger of its scale so far (if it holds earlier tokens of the request) and the least power of two 2^e, e >= -100, with
+ * |x| <= M 2^e for its new values (M = 448 or 127; 0 if they are all 0).  Codes are x / scale to the nearest, ties to even; codes of earlier tokens are
+ * rounded anew when the scale rises (exact for e4m3 but for the smallest values; int8 loses up to a step of the new scale in all).  Codes of the
+ * begun block behind the new tokens are set to 0.  A new value that is not finite makes the block's scale NaN and its codes 0: queries that see any of its tokens
+ * give NaN.  A page may stand in the table of several entries only if none of them writes to it (flat_attn_cache8_fork sees to that).
+ */
+int flat_attn_cache8_write(const flat_cache8* cache, const void* K, const void* V, int B, int N, const int* page_table, int max_pages,
+                           const int* lens, const int* n_new, void* stream);
+
+/*
+ * Fused attention of Nq queries of each batch entry over its tokens in the cache; H / n_heads query heads share a head of the cache (head h of Q
+ * reads head h / (H / n_heads)).
+ *   Q: device, const bf16 [B,H,Nq,d].  O: device, bf16 [B,H,Nq,d].  H: a multiple of n_heads (else FLAT_ERR_SHAPE).
+ *   lens: device, const int [B]: tokens that count, the new ones among them, clamped to [0, max_pages * page_tokens].
+ *   q_lens: device, const int [B], clamped to [0, Nq], or NULL: Nq for every entry.  Rows of O behind an entry's last query are left as they are.
+ *   mask_kind FLAT_MASK_CAUSAL: an entry's queries are the last q_lens[b] of its lens[b] positions, so query i sees token j iff
+ *     j <= i + lens[b] - q_lens[b].  A query that sees no token gives zeros.
+ *   workspace: device, 16-byte aligned, at least flat_attn_fwd_cache8_workspace_bytes() bytes (same B, H, n_heads, Nq, d; max_tokens = max_pages *
+ *     page_tokens), overwritten; may be NULL where that is 0.  It overlaps no other buffer.
+ * Logits, softmax statistics and sums in fp32, probabilities (times the value's scale) rounded to bf16, as flat_attn_fwd.  How the keys of an entry are
+ * divided over workgroups follows from the lengths of the whole batch, so an entry's last bits may change with its neighbours' lengths; the same call gives the same bits.
+ */
+size_t flat_attn_fwd_cache8_workspace_bytes(int B, int H, int n_heads, int Nq, int max_tokens, int d);
+int flat_attn_fwd_cache8(const flat_cache8* cache, const void* Q, void* O, int B, int H, int Nq, const int* page_table, int max_pages,
+                         const int* lens, const int* q_lens, float scale, int mask_kind, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Pages.  A page is held if a row of the page table names it, so rows hold -1 (or another hole) where they have no page.  page_table and new_table: device, int [n_seqs,max_pages];
+ * lens: device, int [n_seqs]; lists: device, const int.  A page's codes and scales of K and V move together, bit for bit.
+ *
+ * flat_attn_cache8_copy_pages: page src[i] to page dst[i], i < n.  A pair with an id outside [0, n_pages), or with src[i] = dst[i], does nothing; of pairs
+ *   with the same destination the last one counts; a pair whose source is the destination of a pair that counts is left out.
+ * flat_attn_cache8_fork: entry children[i] becomes a copy of entry parents[i]: its length, its full pages (shared), and the begun last page (lens no
+ *   multiple of page_tokens), which is copied to page spares[i] so that both can be written to.  The rest of the child's row becomes -1.  A fork is left out, and its child as it was, if an id
+ *   is outside [0, n_seqs), parent and child are the same, a later fork has the same child, the parent is the child of any fork in the list, or it needs its spare and
+ *   that is outside [0, n_pages), the begun page itself or a later fork's spare.  Spares are for pages that no row holds.
+ * flat_attn_cache8_free: the rows seqs[i] of the page table become -1 and their lens 0 (ids outside [0, n_seqs) do nothing); then unused[0 .. *n_unused) are
+ *   the pages that no row holds, ascending, and the rest of unused[n_pages] is -1.  n = 0 only lists.  n_pages is at most FLAT_CACHE8_MAX_LISTED_PAGES.
+ * flat_attn_cache8_compact: held pages, *n_used of them, move to ids 0 .. *n_used - 1: those from *n_used on, in ascending order, to the ids below that nobody
+ *   holds, in ascending order; the others stay.  new_table (which may be page_table itself) names the pages where they are then; holes stay as they are.  workspace:
+ *   device, 4-byte aligned, at least flat_attn_cache8_compact_workspace_bytes() bytes, overwritten.  n_pages at most FLAT_CACHE8_MAX_LISTED_PAGES.
+ */
+#define FLAT_CACHE8_MAX_LISTED_PAGES (1 << 20)
+int flat_attn_cache8_copy_pages(const flat_cache8* cache, const int* src, const int* dst, int n, void* stream);
+int flat_attn_cache8_fork(const flat_cache8* cache, int* page_table, int max_pages, int n_seqs, int* lens, const int* parents,
+                          const int* children, const int* spares, int n, void* stream);
+int flat_attn_cache8_free(int* page_table, int max_pages, int n_seqs, int* lens, const int* seqs, int n, int n_pages, int* unused,
+                          int* n_unused, void* stream);
+size_t flat_attn_cache8_compact_workspace_bytes(int n_pages);
+int flat_attn_cache8_compact(const flat_cache8* cache, const int* page_table, int* new_table, int max_pages, int n_seqs, int* n_used,
+                             void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a flat_status value (static storage, never NULL). */
 const char* flat_attn_status_string(int status);

@@ -35,6 +35,11 @@ class FlatTileShape(ctypes.Structure):
         return {n: int(getattr(self, n)) for n, _ in self._fields_}
 
 
+class FlatCache8Struct(ctypes.Structure):
+    """flat_cache8 of the header, field for field."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [(n, ctypes.c_int) for n in ("n_pages", "n_heads", "page_tokens", "d", "format")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -121,6 +126,20 @@ def load_library():
     lib.flat_attn_tile_shape_default.argtypes = [i, i, i, i, i]
     lib.flat_attn_fwd_tile.restype = i
     lib.flat_attn_fwd_tile.argtypes = [vp, vp, vp, vp, i, i, i, i, f, i, i, vp]
+    cache = ctypes.POINTER(FlatCache8Struct)
+    for name, restype, argtypes in (
+            ("flat_attn_rope", i, [vp, vp, i, vp, vp, i, i, i, i, i, i, i, vp, vp, f, i, vp]),
+            ("flat_attn_rope_freqs", i, [vp, i] + [ctypes.c_double, i] + [ctypes.c_double] * 4),
+            ("flat_attn_cache8_write", i, [cache, vp, vp, i, i, vp, i, vp, vp, vp]),
+            ("flat_attn_fwd_cache8_workspace_bytes", sz, [i] * 6),
+            ("flat_attn_fwd_cache8", i, [cache, vp, vp, i, i, i, vp, i, vp, vp, f, i, vp, sz, vp]),
+            ("flat_attn_cache8_copy_pages", i, [cache, vp, vp, i, vp]),
+            ("flat_attn_cache8_fork", i, [cache, vp, i, i, vp, vp, vp, vp, i, vp]),
+            ("flat_attn_cache8_free", i, [vp, i, i, vp, vp, i, i, vp, vp, vp]),
+            ("flat_attn_cache8_compact_workspace_bytes", sz, [i]),
+            ("flat_attn_cache8_compact", i, [cache, vp, vp, i, i, vp, vp, sz, vp])):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = restype, argtypes
     lib.flat_attn_status_string.restype = ctypes.c_char_p
     lib.flat_attn_status_string.argtypes = [i]
     lib.flat_attn_version.restype = i
