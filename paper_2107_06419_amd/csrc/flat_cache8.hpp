@@ -53,12 +53,13 @@ hipError_t launch_cache8_compact(const flat_cache8& c, const int* page_table, in
 // Attention over the cache (flat_cache8_fwd.hip).  A row block is rows_per_block of the Nq * (H / heads) rows that share a head of the cache;
 // an entry is a row block of a batch entry, and its keys are divided over one or more units, a workgroup per unit and head.
 struct Cache8Plan {
-    int rows_per_block;
-    int row_blocks;   // per batch entry, for Nq queries
-    int entries;      // B * row_blocks
-    int target;       // units that the launch aims at over all entries (0: every entry is one unit)
-    int least_tiles;  // of 32 keys that a unit has, unless its entry has fewer
-    int max_units;    // no launch has more
+    int rows_per_block;  // 32: wavefronts share the keys of a block's rows; more: each has 32 rows of its own
+    int row_blocks;      // per batch entry, for Nq queries
+    int entries;         // B * row_blocks
+    int tile_keys;       // what keys are divided by: a power of two
+    int aim, limit;      // units aimed at over all entries, and the most there are (per head of the cache); 0: every entry is one unit
+    int least_tiles;     // that a unit has, unless its entry has fewer
+    size_t parts_at;     // bytes of the workspace before the units' partial results
     size_t workspace_bytes;
 };
 void cache8_plan(int B, int H, int heads, int Nq, int max_tokens, int d, Cache8Plan* out);  // host arithmetic only

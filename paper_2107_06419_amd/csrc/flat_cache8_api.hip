@@ -107,7 +107,8 @@ static bool attend_plan(int B, int H, int heads, int Nq, long long max_tokens, i
     if (rows > kMaxInt / 2 || (long long)B * heads > kMaxInt / 2 / rows) return false;  // the grids: one workgroup per row in the merge
     if ((unsigned long long)Nq * (unsigned)d * 2u > 0xffffffffULL) return false;
     flat::cache8_plan(B, H, heads, Nq, (int)max_tokens, d, plan);
-    return (long long)plan->max_units * heads <= kMaxInt;
+    const long long grid = plan->limit ? plan->limit : plan->entries;
+    return grid * heads <= kMaxInt - 7;
 }
 
 size_t flat_attn_fwd_cache8_workspace_bytes(int B, int H, int n_heads, int Nq, int max_tokens, int d) {

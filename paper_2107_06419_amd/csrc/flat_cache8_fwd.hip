@@ -1,90 +1,364 @@
 // Attention over the paged 8-bit cache.  See flat_cache8.hpp for the layout that this rests on.
 //
-// Few rows.  A workgroup has up to 32 of the Nq * group rows that share a head of the cache, and its four wavefronts take the unit's
-// tiles of 32 keys in turn.  A tile is S^T = K Q^T and O^T += V^T P^T on the 32 x 32 x 16 bf16 MFMAs, with K and V widened from their codes in
-// registers: no LDS in the loop, no barrier.  Row m of the K operand is block (m / 4) % 2, token 4 (m / 8) + m % 4, so that the accumulator of a
-// lane in wave half h holds the 16 tokens of block h in order: exactly the contraction order in which the same half holds V's bytes.  The
-// probabilities go from one MFMA to the other without leaving their lane, and a lane needs the scales of one block only.
+// A tile of 32 keys is S^T = K Q^T and O^T += V^T P^T on the 32 x 32 x 16 bf16 MFMAs.  Row m of the K operand is block (m / 4) % 2, token 4 (m / 8) + m % 4, so
+// that the accumulator of a lane in wave half h holds the 16 tokens of block h in order: exactly the contraction order in which the same half
+// holds V's bytes.  The probabilities go from one MFMA to the other without leaving their lane, and a lane needs the scales of one block only.
 #include "flat_cache8_fwd.hpp"
 
 namespace flat {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kRescaleAbove = 8;  // log2: the reference maximum rises only when a logit is this far above it
+// Where a row of a unit's result goes: O if the unit is its entry's only one, else the workspace.
+template <int D>
+__device__ __forceinline__ bf16* row_of_o(const Cache8Args& a, const CacheEntry& t, int kvh, int row) {
+    const int pos = a.by_group.quotient(row), g = row - pos * a.group;
+    return a.O + ((size_t)(t.b * (size_t)a.H + kvh * a.group + g) * a.Nq + pos) * D;
+}
+template <int D>
+__device__ __forceinline__ float* part_of(const Cache8Args& a, int u, int kvh) {
+    return a.parts + (size_t)(u * (size_t)a.heads + kvh) * ((size_t)a.rows_per_block * (D + 2));
+}
+__device__ __forceinline__ floatx2 four_bf16(const floatx4& y, float by) {
+    floatx2 out;
+    out[0] = __builtin_bit_cast(float, pack_bf16(y[0] * by, y[1] * by));
+    out[1] = __builtin_bit_cast(float, pack_bf16(y[2] * by, y[3] * by));
+    return out;
+}
 
-// What a wavefront knows of the next 32 tiles it takes: lane l has block l % 2 of the (l / 2)-th of them.
-struct BlockInfo {
-    int e;         // block number in the pool, -1 a hole
-    float ks, vs;  // its scales; 0 for a hole
-};
+// ---- Few rows: up to 32 of the Nq * group rows that share a head of the cache.  The four wavefronts of a workgroup take the unit's steps of
+// 32 TPS keys in turn, with K and V widened from their codes in registers: no LDS and no barrier before the end.  What bounds it is the reading of the
+// codes: a wavefront asks for the next step's as soon as this one's are widened, 8 KiB a step at d = 32 to 128, so that 64 KiB a compute unit are on their way.
+constexpr int kWaves = 4;
+
+template <int D>
+constexpr int tiles_per_step() { return D == 32 ? 4 : D == 64 ? 2 : 1; }
 
 template <int D, int FMT>
 __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows_kernel(const Cache8Args a) {
-    constexpr int J = D / 32;        // 16-byte pieces of a K row per wave half, and 32-channel groups of V
-    constexpr int RS = D + 4;        // row stride of the merge buffer, floats: spreads the rows over the banks
+    constexpr int J = D / 32;             // 16-byte pieces of a K row per wave half, and 32-channel groups of V
+    constexpr int TPS = tiles_per_step<D>(), BPS = 2 * TPS, GROUP = 64 / BPS;  // tiles and blocks of a step; steps whose blocks 64 lanes know
+    constexpr int RS = D + 4;             // row stride of the merge buffer, floats: spreads the rows over the banks
     extern __shared__ __align__(16) float lds[];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, col = lane & 31;
     const int id = blockIdx.x, u = a.by_heads.quotient(id), kvh = id - u * a.heads;
 
-    const int chunk = cache_chunk(a, lane);
-    CacheUnit unit{u, u, 1};
-    if (a.target) unit = cache_find_unit(a, u, chunk, lane);
-    if (unit.entry < 0) return;
-    CacheEntry t = cache_entry(a, unit.entry);
+    CacheUnit unit;
+    if (a.limit) {
+        unit = cache_find_unit(a, u, lane);
+        if (unit.e < 0) return;
+    } else {
+        unit.entry = cache_entry(a, u);
+        unit.e = unit.before = u;
+        unit.n = 1;
+    }
+    const CacheEntry& t = unit.entry;
     if (t.row0 >= t.rows) return;
-    const int part = u - unit.before;
-    const int share = (unsigned)t.tiles / (unsigned)unit.n, more = t.tiles - share * unit.n;  // the first `more` parts have one tile more
-    const int tile0 = part * share + min(part, more), tile1 = tile0 + share + (part < more ? 1 : 0);
+    int step0, step1;
+    cache_part(t.tiles, u - unit.before, unit.n, &step0, &step1);
+
+    // blocks of the wavefront's steps first, first + kWaves, ...
+    const int* table = a.page_table + (size_t)t.b * a.max_pages;
+    const int first = step0 + w, n_mine = first < step1 ? (step1 - first + kWaves - 1) / kWaves : 0;
+    const int my_block = BPS * (first + kWaves * (lane / BPS)) + lane % BPS;  // of this lane in the first group
+    auto page_of = [&](int group) __attribute__((always_inline)) {
+        const int blk = my_block + group * (BPS * kWaves * GROUP);
+        return kCacheBlock * blk < t.len ? table[a.by_page_blocks.quotient(blk)] : -1;
+    };
+    auto block_of = [&](int group, int page) __attribute__((always_inline)) {
+        return cache_block(a, kvh, t.len, my_block + group * (BPS * kWaves * GROUP), page);
+    };
+    const int page0 = n_mine ? page_of(0) : -1;
 
     // the rows: row = position * group + query head of the group
-    const int row = t.row0 + col, pos = a.by_group.quotient(row), g = row - pos * a.group;
+    const int row = t.row0 + col, pos = a.by_group.quotient(row);
     const bool has_row = row < t.rows;
-    const size_t q_at = ((size_t)(t.b * (size_t)a.H + kvh * a.group + g) * a.Nq + pos) * D;
     bf16x8 q[2 * J];
 #pragma unroll
     for (int j = 0; j < J; ++j) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             q[2 * j + i] = bf16x8{};
-            if (has_row) q[2 * j + i] = *(const bf16x8*)(a.Q + q_at + 32 * j + 16 * half + 8 * i);
+            if (has_row) q[2 * j + i] = *(const bf16x8*)(row_of_o<D>(a, t, kvh, row) - a.O + a.Q + 32 * j + 16 * half + 8 * i);
         }
     }
     const int seen = !has_row ? t.len : a.causal ? min(max(pos + 1 + t.len - t.q_len, 0), t.len) : t.len;  // keys that this row sees
-    const int all_see = a.causal ? min(max(a.by_group.quotient(t.row0) + 1 + t.len - t.q_len, 0), t.len) : t.len;
+    const int all_see = __builtin_amdgcn_readfirstlane(a.causal ? min(max(a.by_group.quotient(t.row0) + 1 + t.len - t.q_len, 0), t.len) : t.len);
 
-    const int blocks = (t.len + kCacheBlock - 1) / kCacheBlock;
-    const int* table = a.page_table + (size_t)t.b * a.max_pages;
-    const int first = tile0 + w;  // tiles first, first + kWaves, ...
-    auto page_of = [&](int group) __attribute__((always_inline)) {  // page of this lane's block in the group-th 32 tiles, -1 a hole
-        const int blk = 2 * (first + kWaves * (32 * group + (lane >> 1))) + (lane & 1);
-        return blk < blocks ? table[a.by_page_blocks.quotient(blk)] : -1;
-    };
-    auto info_of = [&](int group, int page) __attribute__((always_inline)) {
-        const int blk = 2 * (first + kWaves * (32 * group + (lane >> 1))) + (lane & 1);
-        BlockInfo x{-1, 0.f, 0.f};
-        if (blk < blocks && (unsigned)page < (unsigned)a.n_pages) {
-            x.e = (page * a.heads + kvh) * a.page_blocks + blk - a.by_page_blocks.quotient(blk) * a.page_blocks;
-            x.ks = a.ks[x.e] * a.scale_log2;
-            x.vs = a.vs[x.e];
+    CacheBlock now = block_of(0, page0), next = now;
+    int next_page = -1;
+    int now_e = now.e;
+    const uint32_t k_lane = (4 * (col >> 3) + (col & 3)) * 16 + half * 256, v_lane = col * 16;
+    const bool k_second = (col >> 2) & 1;
+    uint4v kc[TPS][J], vc[TPS][J];
+    auto load = [&](const uint8_t* pool, int e, int at, uint32_t mine, bool second, uint4v (&x)[TPS][J]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) {
+            const int e0 = max(__builtin_amdgcn_readlane(e, BPS * at + 2 * t2), 0), e1 = max(__builtin_amdgcn_readlane(e, BPS * at + 2 * t2 + 1), 0);
+            const uint8_t* p = pool + (second ? (size_t)e1 * (16 * D) : (size_t)e0 * (16 * D)) + mine;
+#pragma unroll
+            for (int j = 0; j < J; ++j) x[t2][j] = *(const uint4v*)(p + 512 * j);
         }
+    };
+    auto load_k = [&](int at) __attribute__((always_inline)) { load(a.k, now_e, at, k_lane, k_second, kc); };
+    auto load_v = [&](int at) __attribute__((always_inline)) { load(a.v, now_e, at, v_lane, half, vc); };
+
+    floatx16 o[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
+    RowState st{-INFINITY, 0.f, 0.f};
+
+    if (n_mine > 0) {
+        load_k(0);
+        load_v(0);
+    }
+    for (int i = 0; i < n_mine; ++i) {
+        const int at = i % GROUP;
+        // pages and scales of the next GROUP steps: fetched over these, so that their two round trips are not waited for
+        if (at == 0 && i + GROUP < n_mine) next_page = page_of(i / GROUP + 1);
+        if (at == GROUP / 2 && i + GROUP - GROUP / 2 < n_mine) next = block_of(i / GROUP + 1, next_page);
+        float c[TPS], vs_log2[TPS], vs_inv[TPS];
+        int there[TPS], lack = 0;
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) {
+            const int s0 = BPS * at + 2 * t2, s1 = s0 + 1;
+            const int n0 = __builtin_amdgcn_readlane(now.there, s0), n1 = __builtin_amdgcn_readlane(now.there, s1);
+            lack |= (16 - n0) | (16 - n1);
+            there[t2] = half ? n1 : n0;
+            c[t2] = half ? lane_value(now.ks, s1) : lane_value(now.ks, s0);
+            vs_log2[t2] = half ? lane_value(now.vs_log2, s1) : lane_value(now.vs_log2, s0);
+            vs_inv[t2] = half ? lane_value(now.vs_inv, s1) : lane_value(now.vs_inv, s0);
+        }
+        int hole[TPS];
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) hole[t2] = half ? __builtin_amdgcn_readlane(now.e, BPS * at + 2 * t2 + 1) : __builtin_amdgcn_readlane(now.e, BPS * at + 2 * t2);
+        if (at == GROUP - 1) {
+            now = next;
+            now_e = now.e;
+        }
+
+        floatx16 s[TPS];
+        const int key0 = (first + kWaves * i) * (32 * TPS);
+        const bool edge = key0 + 32 * TPS > all_see || lack != 0;
+        int visible[TPS];
+        float top = -INFINITY;
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[t2][r] = 0.f;
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[t2][j][0], kc[t2][j][1]), q[2 * j], s[t2]);
+                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[t2][j][2], kc[t2][j][3]), q[2 * j + 1], s[t2]);
+                if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);  // the widening takes registers: not all of it at once
+            }
+        }
+        // K's registers are free: the next step's codes into them, and V's below
+        if (i + 1 < n_mine) load_k((i + 1) % GROUP);
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) {
+            visible[t2] = 16;
+            float most;
+            if (edge) {
+                visible[t2] = hole[t2] < 0 ? 0 : min(max(seen - key0 - 32 * t2 - kCacheBlock * half, 0), 16);
+#pragma unroll
+                for (int j = 0; j < J; ++j) vc[t2][j] = clear_behind(vc[t2][j], there[t2]);
+                most = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, r < visible[t2] ? s[t2][r] : -INFINITY);
+                most = most == -INFINITY ? most : most * c[t2];  // a scale of 0 leaves nothing unseen a maximum
+            } else {
+                most = s[t2][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) most = __builtin_fmaxf(most, s[t2][r]);
+                most *= c[t2];
+            }
+            top = __builtin_fmaxf(top, most);
+        }
+        top = halves_max(top);
+        if (__any(top > st.m + kRescaleAbove)) {
+            const float up = __builtin_fmaxf(st.m, top), sub = up == -INFINITY ? 0.f : up;
+            const float by = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.sub - sub);
+            st.l *= by;
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[j][r] *= by;
+            st.m = up;
+            st.sub = sub;
+        }
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) {
+            bf16x8 lo, hi;
+            if (edge) tile_probabilities<true>(s[t2], c[t2], vs_log2[t2], vs_inv[t2], st.sub, visible[t2], &lo, &hi, &st.l);
+            else tile_probabilities<false>(s[t2], c[t2], vs_log2[t2], vs_inv[t2], st.sub, 16, &lo, &hi, &st.l);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[t2][j][0], vc[t2][j][1]), lo, o[j]);
+                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[t2][j][2], vc[t2][j][3]), hi, o[j]);
+                if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (i + 1 < n_mine) load_v((i + 1) % GROUP);
+    }
+    st.l = halves_sum(st.l);
+
+    // the four wavefronts' parts: every one scales its own to the common maximum, then all add up
+    float* stat = lds + kWaves * 32 * RS;  // [kWaves][2][32]
+    if (half == 0) {
+        stat[w * 64 + col] = st.m;
+        stat[w * 64 + 32 + col] = st.l;
+    }
+    __syncthreads();
+    auto joined = [&](int r, float* top, float* sum) __attribute__((always_inline)) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) m = __builtin_fmaxf(m, stat[i * 64 + r]);
+        float l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            const float mi = stat[i * 64 + r], li = stat[i * 64 + 32 + r];
+            l += mi == -INFINITY ? li : li * __builtin_amdgcn_exp2f(mi - m);  // without a maximum the sum is 0, or not a number
+        }
+        *top = m;
+        *sum = l;
+    };
+    float top, sum;
+    joined(col, &top, &sum);
+    const float mine = st.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - top);
+    const int rows = min(t.rows - t.row0, 32);
+    if (col < rows) {
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                floatx4 y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] = o[j][4 * x + r] * mine;
+                *(floatx4*)(lds + (w * 32 + col) * RS + 32 * j + 8 * x + 4 * half) = y;
+            }
+    }
+    __syncthreads();
+    constexpr int Q4 = D / 4;  // 16-byte groups of columns per row
+    float* part = part_of<D>(a, u, kvh);
+    for (int x = tid; x < rows * Q4; x += 64 * kWaves) {
+        const int r = x / Q4, c4 = x - r * Q4;
+        floatx4 y = *(const floatx4*)(lds + r * RS + 4 * c4);
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i) y += *(const floatx4*)(lds + (i * 32 + r) * RS + 4 * c4);
+        if (unit.n > 1) {
+            *(floatx4*)(part + r * D + 4 * c4) = y;
+            continue;
+        }
+        float m, l;
+        joined(r, &m, &l);
+        *(floatx2*)(row_of_o<D>(a, t, kvh, t.row0 + r) + 4 * c4) = four_bf16(y, l == 0.f ? 0.f : 1.0f / l);
+    }
+    if (unit.n > 1 && tid < rows) {
+        part[32 * D + tid] = top;
+        part[32 * D + 32 + tid] = sum;
+    }
+    if (a.limit && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
+}
+
+// ---- More rows: every wavefront has 32 rows of its own and takes all keys of the unit.  The workgroup widens each tile of 64 keys once, in
+// LDS, as the MFMA operands in the order of their lanes (1 KiB each), so that reading and writing them meets no bank twice; while a tile is
+// worked on, the next one's codes are widened and the loads of the one after it are in flight.  One barrier per tile.
+template <int D, int FMT, int NW>
+__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(const Cache8Args a, int blocks_per_xcd) {
+    constexpr int J = D / 32, PAIRS = 4 * J;            // pairs of operands of a tile: K of (sub-tile, j), then V
+    constexpr int MINE = (PAIRS + NW - 1) / NW;         // of a wavefront: pairs w, w + NW, ...
+    constexpr int BUF = PAIRS * 2 * 1024;               // bytes of a tile
+    constexpr int GROUP = 16;                           // tiles whose blocks 64 lanes know
+    extern __shared__ __align__(16) uint8_t smem[];
+    float* scales = (float*)(smem + 2 * BUF);           // [2][64 blocks][4]: ks, vs_log2, vs_inv, tokens there as int (-1: a hole)
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5, col = lane & 31;
+    // units of one batch entry and head follow each other on one XCD: they read the same codes
+    const int id = xcd_logical_block(blockIdx.x, blocks_per_xcd);
+    int u, kvh;
+    CacheUnit unit;
+    if (a.limit) {
+        u = a.by_heads.quotient(id);
+        kvh = id - u * a.heads;
+        unit = cache_find_unit(a, u, lane);
+        if (unit.e < 0) return;
+    } else {
+        const int bh = a.by_row_blocks.quotient(id), b = a.by_heads.quotient(bh);
+        if (b >= a.B) return;
+        kvh = bh - b * a.heads;
+        u = b * a.row_blocks + a.row_blocks - 1 - (id - bh * a.row_blocks);  // later rows see more keys: they go first
+        unit.entry = cache_entry(a, u);
+        unit.e = unit.before = u;
+        unit.n = 1;
+    }
+    const CacheEntry& t = unit.entry;
+    if (t.row0 >= t.rows) return;
+    int tile0, tile1;
+    cache_part(t.tiles, u - unit.before, unit.n, &tile0, &tile1);
+
+    const int* table = a.page_table + (size_t)t.b * a.max_pages;
+    auto page_of = [&](int group) __attribute__((always_inline)) {
+        const int blk = 4 * (tile0 + GROUP * group) + lane;
+        return kCacheBlock * blk < t.len ? table[a.by_page_blocks.quotient(blk)] : -1;
+    };
+    auto block_of = [&](int group, int page) __attribute__((always_inline)) {
+        const CacheBlock x = cache_block(a, kvh, t.len, 4 * (tile0 + GROUP * group) + lane, page);
+        if (w == 0) *(floatx4*)(scales + 4 * (64 * (group & 1) + lane)) = floatx4{x.ks, x.vs_log2, x.vs_inv, __builtin_bit_cast(float, x.e < 0 ? -1 : x.there)};
         return x;
     };
+    CacheBlock now = block_of(0, page_of(0)), next = now;
+    int next_page = -1;
+
+    const int row = t.row0 + 32 * w + col;
+    const bool has_row = row < t.rows;
+    bf16x8 q[2 * J];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            q[2 * j + i] = bf16x8{};
+            if (has_row) q[2 * j + i] = *(const bf16x8*)(row_of_o<D>(a, t, kvh, row) - a.O + a.Q + 32 * j + 16 * half + 8 * i);
+        }
+    auto seen_by = [&](int r) __attribute__((always_inline)) { return a.causal ? min(max(a.by_group.quotient(r) + 1 + t.len - t.q_len, 0), t.len) : t.len; };
+    const int seen = has_row ? seen_by(row) : t.len;
+    const int first_row = t.row0 + 32 * w, last_row = min(first_row + 31, t.rows - 1);
+    const int all_see = __builtin_amdgcn_readfirstlane(seen_by(first_row));                           // keys that every row of this wavefront sees
+    const int any_sees = __builtin_amdgcn_readfirstlane(first_row < t.rows ? seen_by(last_row) : 0);  // and that some row sees: 0 without rows
 
     const uint32_t k_lane = (4 * (col >> 3) + (col & 3)) * 16 + half * 256, v_lane = col * 16;
     const bool k_second = (col >> 2) & 1;
-    uint4v kc[J], vc[J], kn[J], vn[J];
-    auto load = [&](const BlockInfo& x, int at, uint4v* k, uint4v* v) __attribute__((always_inline)) {
-        const int e0 = max(__builtin_amdgcn_readlane(x.e, 2 * at), 0), e1 = max(__builtin_amdgcn_readlane(x.e, 2 * at + 1), 0);
-        const size_t at0 = (size_t)e0 * (16 * D), at1 = (size_t)e1 * (16 * D);
-        const uint8_t* kp = a.k + (k_second ? at1 : at0) + k_lane;
-        const uint8_t* vp = a.v + (half ? at1 : at0) + v_lane;
+    uint4v codes[MINE];
+    auto load = [&](int i) __attribute__((always_inline)) {  // this wavefront's share of tile i of the unit; `now` is the group it lies in
 #pragma unroll
-        for (int j = 0; j < J; ++j) k[j] = *(const uint4v*)(kp + 512 * j);
+        for (int x = 0; x < MINE; ++x) {
+            const int p = w + NW * x;
+            if (PAIRS % NW && p >= PAIRS) continue;
+            const bool is_v = p >= 2 * J;
+            const int sub = (p - (is_v ? 2 * J : 0)) / J, j = (p - (is_v ? 2 * J : 0)) % J, at = 4 * (i % GROUP) + 2 * sub;
+            const int e0 = max(__builtin_amdgcn_readlane(now.e, at), 0), e1 = max(__builtin_amdgcn_readlane(now.e, at + 1), 0);
+            const size_t at0 = (size_t)e0 * (16 * D), at1 = (size_t)e1 * (16 * D);
+            const uint8_t* base = is_v ? a.v + (half ? at1 : at0) + v_lane : a.k + (k_second ? at1 : at0) + k_lane;
+            codes[x] = *(const uint4v*)(base + 512 * j);
+        }
+    };
+    auto widen = [&](int i, int buf) __attribute__((always_inline)) {  // the loaded share into LDS
 #pragma unroll
-        for (int j = 0; j < J; ++j) v[j] = *(const uint4v*)(vp + 512 * j);
+        for (int x = 0; x < MINE; ++x) {
+            const int p = w + NW * x;
+            if (PAIRS % NW && p >= PAIRS) continue;
+            uint4v c = codes[x];
+            if (p >= 2 * J) {
+                const int there = __builtin_bit_cast(int, scales[4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + 2 * ((p - 2 * J) / J) + half) + 3]);
+                if (__any(there < 16)) c = clear_behind(c, there);
+            }
+            uint8_t* to = smem + buf * BUF + p * 2048 + lane * 16;
+            *(bf16x8*)to = codes_to_bf16<FMT>(c[0], c[1]);
+            *(bf16x8*)(to + 1024) = codes_to_bf16<FMT>(c[2], c[3]);
+        }
     };
 
     floatx16 o[J];
@@ -92,211 +366,177 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
     for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
-    float m = -INFINITY, msub = 0.f, l = 0.f;  // reference maximum (log2 units), what is subtracted (0 until there is a maximum), row sum of this half
+    RowState st{-INFINITY, 0.f, 0.f};
 
-    const int n_mine = first < tile1 ? (tile1 - first + kWaves - 1) / kWaves : 0;
-    BlockInfo now{-1, 0.f, 0.f}, next{-1, 0.f, 0.f};
-    int next_page = -1;
-    if (n_mine > 0) {
-        now = info_of(0, page_of(0));
-        load(now, 0, kc, vc);
-    }
-    for (int i = 0; i < n_mine; ++i) {
-        const int at = i & 31;
-        // pages and scales of the next 32 tiles: fetched over this 32, so that their two round trips are not waited for
-        if (at == 0 && i + 32 < n_mine) next_page = page_of((i >> 5) + 1);
-        if (at == 16 && i + 16 < n_mine) next = info_of((i >> 5) + 1, next_page);
-        const int s0 = 2 * at, s1 = 2 * at + 1;
-        const int e0 = __builtin_amdgcn_readlane(now.e, s0), e1 = __builtin_amdgcn_readlane(now.e, s1);
-        const int ks0 = __builtin_amdgcn_readlane(__builtin_bit_cast(int, now.ks), s0), ks1 = __builtin_amdgcn_readlane(__builtin_bit_cast(int, now.ks), s1);
-        const int vs0 = __builtin_amdgcn_readlane(__builtin_bit_cast(int, now.vs), s0), vs1 = __builtin_amdgcn_readlane(__builtin_bit_cast(int, now.vs), s1);
-        const float ks = __builtin_bit_cast(float, half ? ks1 : ks0), vs = __builtin_bit_cast(float, half ? vs1 : vs0);
-        if (at == 31) now = next;
-        if (i + 1 < n_mine) load(now, (i + 1) & 31, kn, vn);
-
-        floatx16 s;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = 0.f;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            s = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[j][0], kc[j][1]), q[2 * j], s);
-            s = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[j][2], kc[j][3]), q[2 * j + 1], s);
-        }
-        const int key0 = (first + kWaves * i) * kCacheTile;
-        float c = ks;
-        int visible = 16;  // of this lane's block, for its row
-        const bool edge = key0 + kCacheTile > all_see || (e0 | e1) < 0;
-        if (edge) {
-            const int e = half ? e1 : e0;
-            visible = e < 0 ? 0 : min(max(seen - key0 - kCacheBlock * half, 0), 16);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = r < visible ? s[r] * c : -INFINITY;
-            c = 1.f;
-            const int there = e < 0 ? 0 : min(max(t.len - key0 - kCacheBlock * half, 0), 16);
-#pragma unroll
-            for (int j = 0; j < J; ++j) vc[j] = clear_behind(vc[j], there);
-        }
-        float top = s[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = __builtin_fmaxf(top, s[r]);
-        top = halves_max(top * c);
-        if (__any(top > m + kRescaleAbove)) {
-            const float up = __builtin_fmaxf(m, top), sub = up == -INFINITY ? 0.f : up;
-            const float f = __builtin_amdgcn_exp2f(msub - sub);
-            const float by = m == -INFINITY ? 0.f : f;
-            l *= by;
-#pragma unroll
-            for (int j = 0; j < J; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[j][r] *= by;
-            m = up;
-            msub = sub;
-        }
-        float p[16];
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, -msub));
-            l += p[r];
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) p[r] *= vs;
-        if (edge) {  // a block whose scale is NaN is one only for the rows that see it
-#pragma unroll
-            for (int r = 0; r < 16; ++r) p[r] = r < visible ? p[r] : 0.f;
-        }
-        uint4v plo, phi;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            plo[r] = pack_bf16(p[2 * r], p[2 * r + 1]);
-            phi[r] = pack_bf16(p[8 + 2 * r], p[9 + 2 * r]);
-        }
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[j][0], vc[j][1]), __builtin_bit_cast(bf16x8, plo), o[j]);
-            o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[j][2], vc[j][3]), __builtin_bit_cast(bf16x8, phi), o[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < J; ++j) kc[j] = kn[j], vc[j] = vn[j];
-    }
-    l = halves_sum(l);
-
-    // the four wavefronts' parts: every one scales its own to the common maximum, then a quarter of the columns is added up by each
-    float* stat = lds + kWaves * 32 * RS;  // [kWaves][2][32]
-    if (half == 0) {
-        stat[w * 64 + col] = m;
-        stat[w * 64 + 32 + col] = l;
+    const int n = tile1 - tile0;
+    if (n > 0) load(0);
+    __syncthreads();  // the scales of the first group
+    if (n > 0) {
+        widen(0, 0);
+        if (n > 1) load(1);
     }
     __syncthreads();
-    float top = -INFINITY, L = 0.f;
+    for (int i = 0; i < n; ++i) {
+        const int buf = i & 1, at = i % GROUP;
+        // what the next group's blocks are: pages at the start of this one, scales in its middle; its first tile is loaded two tiles ahead
+        if (at == 0 && i + GROUP < n) next_page = page_of(i / GROUP + 1);
+        if (at == GROUP / 2 && i + GROUP - GROUP / 2 < n) next = block_of(i / GROUP + 1, next_page);
+        if (i + 1 < n) widen(i + 1, buf ^ 1);
+        if (at == GROUP - 2) now = next;
+        if (i + 2 < n) load(i + 2);
+        const int key0 = (tile0 + i) * 64;
+        if (key0 < any_sees) {
+            const uint8_t* frag = smem + buf * BUF + lane * 16;
+            const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * at + half);
+            floatx16 s[2];
+            floatx4 x[2];
+            int there[2];
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) top = __builtin_fmaxf(top, stat[i * 64 + col]);
-    const float sub = top == -INFINITY ? 0.f : top;
+            for (int b = 0; b < 2; ++b) {
+                x[b] = *(const floatx4*)(sc + 8 * b);
+                const float last = x[b][3];  // (the bits of a vector's element taken directly would be those of its first)
+                there[b] = __builtin_bit_cast(int, last);
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        const float mi = stat[i * 64 + col], li = stat[i * 64 + 32 + col];
-        L += mi == -INFINITY ? li : li * __builtin_amdgcn_exp2f(mi - sub);  // a part that saw no key has l = 0
-    }
-    const float mine = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - sub);
+                for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-            floatx4 y;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = o[j][4 * x + r] * mine;
-            *(floatx4*)(lds + (w * 32 + col) * RS + 32 * j + 8 * x + 4 * half) = y;
-        }
-    __syncthreads();
-    constexpr int Q4 = D / 4;  // 16-byte groups of columns per row
-    const int rows = min(t.rows - t.row0, 32);
-    if (unit.n == 1) {
-        for (int x = tid; x < rows * Q4; x += 64 * kWaves) {
-            const int r = x / Q4, c4 = x - r * Q4;
-            floatx4 y = *(const floatx4*)(lds + r * RS + 4 * c4);
-#pragma unroll
-            for (int i = 1; i < kWaves; ++i) y += *(const floatx4*)(lds + (i * 32 + r) * RS + 4 * c4);
-            float Lr = 0.f, tr = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) tr = __builtin_fmaxf(tr, stat[i * 64 + r]);
-            const float sr = tr == -INFINITY ? 0.f : tr;
-#pragma unroll
-            for (int i = 0; i < kWaves; ++i) {
-                const float mi = stat[i * 64 + r], li = stat[i * 64 + 32 + r];
-                Lr += mi == -INFINITY ? li : li * __builtin_amdgcn_exp2f(mi - sr);
+                for (int j = 0; j < 2 * J; ++j) s[b] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + (b * J * 2 + j) * 1024), q[j], s[b]);
             }
-            const float inv = Lr == 0.f ? 0.f : 1.0f / Lr;
-            const int rr = t.row0 + r, p = a.by_group.quotient(rr), gg = rr - p * a.group;
-            floatx2 out;
-            out[0] = __builtin_bit_cast(float, pack_bf16(y[0] * inv, y[1] * inv));
-            out[1] = __builtin_bit_cast(float, pack_bf16(y[2] * inv, y[3] * inv));
-            *(floatx2*)(a.O + ((size_t)(t.b * (size_t)a.H + kvh * a.group + gg) * a.Nq + p) * D + 4 * c4) = out;
-        }
-    } else {
-        float* part_ws = a.ws + (size_t)(u * (size_t)a.heads + kvh) * (32 * (D + 2));
-        for (int x = tid; x < rows * Q4; x += 64 * kWaves) {
-            const int r = x / Q4, c4 = x - r * Q4;
-            floatx4 y = *(const floatx4*)(lds + r * RS + 4 * c4);
+            int visible[2];
+            float top = -INFINITY;
+            const bool edge = key0 + 64 > all_see || __any((there[0] | there[1]) < 0);
 #pragma unroll
-            for (int i = 1; i < kWaves; ++i) y += *(const floatx4*)(lds + (i * 32 + r) * RS + 4 * c4);
-            *(floatx4*)(part_ws + r * D + 4 * c4) = y;
+            for (int b = 0; b < 2; ++b) {
+                float most = -INFINITY;
+                visible[b] = 16;
+                if (edge) {
+                    visible[b] = there[b] < 0 ? 0 : min(max(seen - key0 - 32 * b - kCacheBlock * half, 0), 16);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, r < visible[b] ? s[b][r] : -INFINITY);
+                    most = most == -INFINITY ? most : most * x[b][0];
+                } else {
+                    most = s[b][0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) most = __builtin_fmaxf(most, s[b][r]);
+                    most *= x[b][0];
+                }
+                top = __builtin_fmaxf(top, most);
+            }
+            top = halves_max(top);
+            if (__any(top > st.m + kRescaleAbove)) {
+                const float up = __builtin_fmaxf(st.m, top), sub = up == -INFINITY ? 0.f : up;
+                const float by = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.sub - sub);
+                st.l *= by;
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[j][r] *= by;
+                st.m = up;
+                st.sub = sub;
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                bf16x8 p[2];
+                if (edge) tile_probabilities<true>(s[b], x[b][0], x[b][1], x[b][2], st.sub, visible[b], &p[0], &p[1], &st.l);
+                else tile_probabilities<false>(s[b], x[b][0], x[b][1], x[b][2], st.sub, 16, &p[0], &p[1], &st.l);
+#pragma unroll
+                for (int j = 0; j < 2 * J; ++j) o[j / 2] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + ((2 + b) * J * 2 + j) * 1024), p[j & 1], o[j / 2]);
+            }
         }
-        if (w == 0 && half == 0 && col < rows) {
-            part_ws[32 * D + col] = top;
-            part_ws[32 * D + 32 + col] = L;
+        __syncthreads();
+    }
+    st.l = halves_sum(st.l);
+    if (a.limit && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
+    if (!has_row) return;
+    if (unit.n == 1) {
+        const float by = st.l == 0.f ? 0.f : 1.0f / st.l;
+        bf16* to = row_of_o<D>(a, t, kvh, row) + 4 * half;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) *(floatx2*)(to + 32 * j + 8 * x) = four_bf16(floatx4{o[j][4 * x], o[j][4 * x + 1], o[j][4 * x + 2], o[j][4 * x + 3]}, by);
+    } else {
+        float *part = part_of<D>(a, u, kvh), *to = part + (32 * w + col) * D + 4 * half, *stat = part + 32 * NW * D + 32 * w + col;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) *(floatx4*)(to + 32 * j + 8 * x) = floatx4{o[j][4 * x], o[j][4 * x + 1], o[j][4 * x + 2], o[j][4 * x + 3]};
+        if (half == 0) {
+            stat[0] = st.m;
+            stat[32 * NW] = st.l;
         }
     }
 }
 
-// Puts the parts of the rows together whose entry was divided: one workgroup per row of Q.
-constexpr int kMergeThreads = 256;
-template <int D>
-__global__ __launch_bounds__(kMergeThreads) void cache8_merge_kernel(const Cache8Args a, const Divisor by_rows, int rows_per_b) {
-    constexpr int Q4 = D / 4, LANES = kMergeThreads / Q4;
-    __shared__ floatx4 red[kMergeThreads];
-    __shared__ float wts[kMergeThreads], stat[2][kMergeThreads / 64];
+// ---- Puts the parts of a row together whose entry was divided: THREADS threads per row and COLS columns.  M = max m_s, O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.
+// A chain of round trips (the entry's units, then statistics and results together), so the first results are fetched before their weights are known.
+template <int D, int THREADS, int COLS>
+__global__ __launch_bounds__(THREADS) void cache8_merge_kernel(const Cache8Args a, const Divisor by_rows, int rows_per_b) {
+    constexpr int Q4 = COLS / 4, LANES = THREADS / Q4, WAVES = THREADS / 64, AHEAD = 4;
+    __shared__ floatx4 red[THREADS];
+    __shared__ float wts[THREADS], stat[2][WAVES];
     const int tid = threadIdx.x, lane = tid & 63;
-    // blockIdx = (b * heads + head of the cache) * rows_per_b + row
+    // blockIdx.x = (b * heads + head of the cache) * rows_per_b + row
     const int bh = by_rows.quotient(blockIdx.x), row = blockIdx.x - bh * rows_per_b;
     const int b = a.by_heads.quotient(bh), kvh = bh - b * a.heads;
-    const int rb = row / 32, e = b * a.row_blocks + rb, r = row - 32 * rb;
-    const int chunk = cache_chunk(a, lane);
-    const CacheEntry t = cache_entry(a, e);
-    if (row >= t.rows) return;
-    const CacheUnit unit = cache_units_of(a, e, chunk, lane);
-    if (unit.n == 1) return;
-    const size_t stride = (size_t)a.heads * (32 * (D + 2));
-    const float* base = a.ws + ((size_t)unit.before * a.heads + kvh) * (32 * (D + 2));
-    const int c4 = tid % Q4, first = tid / Q4;
+    const int rb = row / a.rows_per_block, e = b * a.row_blocks + rb, r = row - a.rows_per_block * rb;
+    const int2 unit = a.units[e];  // unset where the entry has no rows
+    const int q_len = a.q_lens ? min(max(a.q_lens[b], 0), a.Nq) : a.Nq;
+    if (row >= q_len * a.group || unit.y == 1) return;
+    const int n = unit.y;
+    const size_t size = (size_t)a.rows_per_block * (D + 2), stride = size * a.heads;
+    const float* base = a.parts + ((size_t)unit.x * a.heads + kvh) * size;
+    const float* m_of = base + (size_t)a.rows_per_block * D + r;
+    const int c4 = tid % Q4, first = tid / Q4 < LANES ? tid / Q4 : n;  // d = 96: some threads have no column
+    const float* o_of = base + (size_t)r * D + COLS * blockIdx.y + 4 * c4;
 
-    float top = -INFINITY;
-    for (int s = tid; s < unit.n; s += kMergeThreads) top = __builtin_fmaxf(top, base[s * stride + 32 * D + r]);
+    floatx4 ahead[AHEAD];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, o));
-    if (lane == 0) stat[0][tid >> 6] = top;
-    __syncthreads();
-    top = __builtin_fmaxf(__builtin_fmaxf(stat[0][0], stat[0][1]), __builtin_fmaxf(stat[0][2], stat[0][3]));
-    const float sub = top == -INFINITY ? 0.f : top;
-
+    for (int i = 0; i < AHEAD; ++i) {
+        ahead[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (first + i * LANES < n) ahead[i] = *(const floatx4*)(o_of + (size_t)(first + i * LANES) * stride);
+    }
+    float top = -INFINITY, m0 = -INFINITY, l0 = 0.f;
+    if (tid < n) {
+        m0 = m_of[tid * stride];
+        l0 = m_of[tid * stride + a.rows_per_block];
+    }
+    top = m0;
+    for (int s = tid + THREADS; s < n; s += THREADS) top = __builtin_fmaxf(top, m_of[s * stride]);
+    top = wave_max(top);
+    if (WAVES > 1) {
+        if (lane == 0) stat[0][tid >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) top = __builtin_fmaxf(top, stat[0][i]);
+    }
     floatx4 acc{0.f, 0.f, 0.f, 0.f};
     float L = 0.f;
-    for (int s0 = 0; s0 < unit.n; s0 += kMergeThreads) {
-        if (s0 + tid < unit.n) {
-            const float* p = base + (s0 + tid) * stride;
-            const float ms = p[32 * D + r], ls = p[32 * D + 32 + r];
-            const float wt = ms == -INFINITY ? (ls == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ms - sub);  // no key seen: nothing; a NaN stays one
+    for (int s0 = 0; s0 < n; s0 += THREADS) {
+        if (s0 + tid < n) {
+            if (s0) {
+                m0 = m_of[(s0 + tid) * stride];
+                l0 = m_of[(s0 + tid) * stride + a.rows_per_block];
+            }
+            const float wt = m0 == -INFINITY ? (l0 == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m0 - top);  // no key seen: nothing; what is no number stays so
             wts[tid] = wt;
-            L += wt * ls;
+            L += wt * l0;
         }
         __syncthreads();
-        const int n = min(unit.n - s0, kMergeThreads);
-        if (first < LANES) {
-#pragma unroll 4
-            for (int s = first; s < n; s += LANES) {
-                const floatx4 y = *(const floatx4*)(base + (s0 + s) * stride + r * D + 4 * c4);
-                const float wt = wts[s];
-                if (wt != 0.f) acc += y * wt;
-            }
+        auto add = [&](int s, const floatx4& y) __attribute__((always_inline)) {
+            const float wt = wts[s];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] = wt == 0.f ? acc[i] : acc[i] + wt * y[i];
+        };
+        const int end = min(n - s0, THREADS);
+        int s = first;
+        if (s0 == 0) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (first + i * LANES < end) add(first + i * LANES, ahead[i]);
+            s = first + AHEAD * LANES;
         }
+#pragma unroll 4
+        for (; s < end; s += LANES) add(s, *(const floatx4*)(o_of + (size_t)(s0 + s) * stride));
         __syncthreads();
     }
 #pragma unroll
@@ -305,48 +545,82 @@ __global__ __launch_bounds__(kMergeThreads) void cache8_merge_kernel(const Cache
     red[tid] = acc;
     __syncthreads();
     if (tid >= Q4) return;
-    L = (stat[1][0] + stat[1][1]) + (stat[1][2] + stat[1][3]);
+    L = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) L += stat[1][i];
     for (int k = 1; k < LANES; ++k) acc += red[k * Q4 + c4];
-    const float inv = L == 0.f ? 0.f : 1.0f / L;
     const int p = a.by_group.quotient(row), g = row - p * a.group;
-    floatx2 out;
-    out[0] = __builtin_bit_cast(float, pack_bf16(acc[0] * inv, acc[1] * inv));
-    out[1] = __builtin_bit_cast(float, pack_bf16(acc[2] * inv, acc[3] * inv));
-    *(floatx2*)(a.O + ((size_t)(b * (size_t)a.H + kvh * a.group + g) * a.Nq + p) * D + 4 * c4) = out;
+    *(floatx2*)(a.O + ((size_t)(b * (size_t)a.H + kvh * a.group + g) * a.Nq + p) * D + COLS * blockIdx.y + 4 * c4) = four_bf16(acc, L == 0.f ? 0.f : 1.0f / L);
 }
 
 template <int D, int FMT>
-hipError_t launch(const Cache8Args& args, const Cache8Plan& plan, hipStream_t stream) {
+hipError_t launch_few(const Cache8Args& args, hipStream_t stream) {
     static std::atomic<uint64_t> lds_allowed{0};
     constexpr int lds = (kWaves * 32 * (D + 4) + kWaves * 64) * (int)sizeof(float);
-    hipError_t e = allow_dynamic_lds((const void*)cache8_few_rows_kernel<D, FMT>, lds, &lds_allowed);
+    const hipError_t e = allow_dynamic_lds((const void*)cache8_few_rows_kernel<D, FMT>, lds, &lds_allowed);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((cache8_few_rows_kernel<D, FMT>), dim3((unsigned)plan.max_units * (unsigned)args.heads), dim3(64 * kWaves), lds, stream, args);
-    e = hipGetLastError();
-    if (e != hipSuccess || plan.target == 0) return e;
-    const int rows = args.Nq * args.group;
-    hipLaunchKernelGGL((cache8_merge_kernel<D>), dim3((unsigned)(args.B * args.heads) * (unsigned)rows), dim3(kMergeThreads), 0, stream, args, Divisor(rows), rows);
+    const unsigned units = (unsigned)(args.limit ? args.limit : args.entries);
+    hipLaunchKernelGGL((cache8_few_rows_kernel<D, FMT>), dim3(units * (unsigned)args.heads), dim3(64 * kWaves), lds, stream, args);
+    return hipGetLastError();
+}
+
+template <int D, int FMT, int NW>
+hipError_t launch_rows(const Cache8Args& args, hipStream_t stream) {
+    static std::atomic<uint64_t> lds_allowed{0};
+    constexpr int lds = 2 * (D / 32) * 4 * 2048 + 2 * 64 * 16;
+    const hipError_t e = allow_dynamic_lds((const void*)cache8_rows_kernel<D, FMT, NW>, lds, &lds_allowed);
+    if (e != hipSuccess) return e;
+    const int per_xcd = (int)(((long long)(args.limit ? args.limit : args.entries) * args.heads + 7) / 8);
+    hipLaunchKernelGGL((cache8_rows_kernel<D, FMT, NW>), dim3((unsigned)per_xcd * 8u), dim3(64 * NW), lds, stream, args, per_xcd);
     return hipGetLastError();
 }
 
 template <int D>
-hipError_t launch(const Cache8Args& args, int format, const Cache8Plan& plan, hipStream_t stream) {
-    return format == FLAT_CACHE8_E4M3 ? launch<D, FLAT_CACHE8_E4M3>(args, plan, stream) : launch<D, FLAT_CACHE8_INT8>(args, plan, stream);
+hipError_t launch_merge(const Cache8Args& args, hipStream_t stream) {
+    const int rows = args.Nq * args.group;
+    const unsigned grid = (unsigned)(args.B * args.heads) * (unsigned)rows;
+    if (args.limit <= 4 * args.entries) hipLaunchKernelGGL((cache8_merge_kernel<D, 64, D>), dim3(grid), dim3(64), 0, stream, args, Divisor(rows), rows);
+    else hipLaunchKernelGGL((cache8_merge_kernel<D, 256, 32>), dim3(grid, D / 32), dim3(256), 0, stream, args, Divisor(rows), rows);
+    return hipGetLastError();
+}
+
+template <int D, int FMT>
+hipError_t launch(const Cache8Args& args, hipStream_t stream) {
+    hipError_t e;
+    switch (args.rows_per_block) {
+        case 32: e = launch_few<D, FMT>(args, stream); break;
+        case 64:
+            if constexpr (D != 256) {  // (two wavefronts would have 16 operand pairs of a tile each on their way: too many registers)
+                e = launch_rows<D, FMT, 2>(args, stream);
+                break;
+            }
+            [[fallthrough]];
+        default: e = launch_rows<D, FMT, 4>(args, stream); break;
+    }
+    return e != hipSuccess || args.limit == 0 ? e : launch_merge<D>(args, stream);
+}
+
+template <int D>
+hipError_t launch(const Cache8Args& args, int format, hipStream_t stream) {
+    return format == FLAT_CACHE8_E4M3 ? launch<D, FLAT_CACHE8_E4M3>(args, stream) : launch<D, FLAT_CACHE8_INT8>(args, stream);
 }
 
 }  // namespace
 
 hipError_t launch_cache8_fwd(const flat_cache8& c, const Cache8Attend& a, const Cache8Plan& plan, hipStream_t stream) {
-    Cache8Args args{(const uint8_t*)c.k, (const uint8_t*)c.v, c.k_scale, c.v_scale, (const bf16*)a.Q, (bf16*)a.O, a.page_table, a.lens, a.q_lens,
-                    a.workspace, c.n_pages, c.n_heads, a.max_pages, a.max_pages * c.page_tokens, a.B, a.H, a.Nq, a.H / c.n_heads, a.scale * kLog2e, a.causal,
-                    plan.rows_per_block, plan.row_blocks, plan.entries, plan.target, plan.least_tiles, Divisor(c.n_heads), Divisor(a.H / c.n_heads),
-                    Divisor(plan.row_blocks), Divisor(c.page_tokens / kCacheBlock), c.page_tokens / kCacheBlock};
+    int shift = 0;
+    while (1 << shift < plan.tile_keys) ++shift;
+    const Cache8Args args{(const uint8_t*)c.k, (const uint8_t*)c.v, c.k_scale, c.v_scale, (const bf16*)a.Q, (bf16*)a.O, a.page_table, a.lens, a.q_lens,
+                          (int2*)a.workspace, (float*)((char*)a.workspace + plan.parts_at), c.n_pages, c.n_heads, a.max_pages, a.max_pages * c.page_tokens,
+                          a.B, a.H, a.Nq, a.H / c.n_heads, a.scale * kLog2e, a.causal, plan.rows_per_block, plan.row_blocks, plan.entries, shift, plan.aim,
+                          plan.limit, plan.least_tiles, Divisor(c.n_heads), Divisor(a.H / c.n_heads), Divisor(plan.row_blocks),
+                          Divisor(c.page_tokens / kCacheBlock), c.page_tokens / kCacheBlock};
     switch (c.d) {
-        case 32: return launch<32>(args, c.format, plan, stream);
-        case 64: return launch<64>(args, c.format, plan, stream);
-        case 96: return launch<96>(args, c.format, plan, stream);
-        case 128: return launch<128>(args, c.format, plan, stream);
-        case 256: return launch<256>(args, c.format, plan, stream);
+        case 32: return launch<32>(args, c.format, stream);
+        case 64: return launch<64>(args, c.format, stream);
+        case 96: return launch<96>(args, c.format, stream);
+        case 128: return launch<128>(args, c.format, stream);
+        case 256: return launch<256>(args, c.format, stream);
         default: return hipErrorInvalidValue;
     }
 }

@@ -6,8 +6,6 @@
 
 namespace flat {
 
-constexpr int kCacheTile = 2 * kCacheBlock;  // keys of a step: one 32 x 32 logit tile
-
 // Kernel arguments: geometry, and quotients by launch-time divisors.
 struct Cache8Args {
     const uint8_t *k, *v;
@@ -15,106 +13,172 @@ struct Cache8Args {
     const bf16* Q;
     bf16* O;
     const int *page_table, *lens, *q_lens;
-    float* ws;
+    int2* units;  // workspace of a launch that divides entries: of every entry the units before it and its own,
+    float* parts; // and the units' partial results
     int n_pages, heads, max_pages, max_tokens;
     int B, H, Nq, group;  // group = H / heads
     float scale_log2;
     int causal;
-    int rows_per_block, row_blocks, entries, target, least_tiles;
+    int rows_per_block, row_blocks, entries, tile_shift, aim, limit, least_tiles;
     Divisor by_heads, by_group, by_row_blocks, by_page_blocks;
     int page_blocks;
 };
 
 // One entry of a launch: a row block of a batch entry, with the lengths it goes by.
 struct CacheEntry {
-    int b, row0, rows, len, q_len;  // rows: that the entry has in all (q_len * group)
-    int tiles;                      // of kCacheTile keys that any of its rows sees
+    int b, row0, len, q_len;
+    int rows;   // that the batch entry has in all (q_len * group)
+    int tiles;  // of 2^tile_shift keys that any row of the block sees
 };
 
-__device__ __forceinline__ CacheEntry cache_entry(const Cache8Args& a, int e) {
+__device__ __forceinline__ CacheEntry cache_entry_of(const Cache8Args& a, int e, int len, int q_len) {
     CacheEntry t;
     t.b = a.by_row_blocks.quotient(e);
     t.row0 = (e - t.b * a.row_blocks) * a.rows_per_block;
-    t.len = min(max(a.lens[t.b], 0), a.max_tokens);
-    t.q_len = a.q_lens ? min(max(a.q_lens[t.b], 0), a.Nq) : a.Nq;
-    t.rows = t.q_len * a.group;
-    int seen = t.len;
+    t.len = len;
+    t.q_len = q_len;
+    t.rows = q_len * a.group;
+    int seen = len;
     if (a.causal) {  // what the last row of the block sees
         const int last = a.by_group.quotient(max(min(t.rows, t.row0 + a.rows_per_block) - 1, 0));
-        seen = min(max(last + 1 + t.len - t.q_len, 0), t.len);
+        seen = min(max(last + 1 + len - q_len, 0), len);
     }
-    t.tiles = (seen + kCacheTile - 1) / kCacheTile;
+    t.tiles = (int)(((unsigned)seen + (1u << a.tile_shift) - 1u) >> a.tile_shift);
     return t;
 }
-
-// Units of an entry: one at least if it has rows (they have to be written), each of `chunk` tiles at most.
-__device__ __forceinline__ int cache_units(const CacheEntry& t, int chunk) {
-    if (t.row0 >= t.rows) return 0;
-    return chunk == 0 ? 1 : max((int)(((unsigned)t.tiles + (unsigned)chunk - 1u) / (unsigned)chunk), 1);
+__device__ __forceinline__ CacheEntry cache_entry(const Cache8Args& a, int e) {
+    const int b = a.by_row_blocks.quotient(e);
+    const int len = min(max(a.lens[b], 0), a.max_tokens), q_len = a.q_lens ? min(max(a.q_lens[b], 0), a.Nq) : a.Nq;
+    return cache_entry_of(a, e, len, q_len);
 }
 
-__device__ __forceinline__ unsigned long long wave_sum_u64(unsigned long long x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+// Inclusive sums over the lanes of a wavefront: within rows of 16 lanes, then the rows' totals carried on.
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // from the lane 1, 2, 4, 8 before, in the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next one (rows 1 and 3)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
     return x;
 }
+__device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
 
-// Tiles of a unit: the keys of all entries over the units aimed at, so that long entries get more units than short ones whatever
-// the lengths, which only the device knows; 0: entries are not divided.
-__device__ __forceinline__ int cache_chunk(const Cache8Args& a, int lane) {
-    if (a.target == 0) return 0;
-    unsigned long long total = 0;
-    for (int e = lane; e < a.entries; e += 64) {
-        const CacheEntry t = cache_entry(a, e);
-        total += t.row0 < t.rows ? t.tiles : 0;
-    }
-    total = wave_sum_u64(total) + (unsigned)a.target - 1u;
-    const int chunk = total >> 32 ? (int)(total / (unsigned)a.target) : (int)((unsigned)total / (unsigned)a.target);
-    return max(__builtin_amdgcn_readfirstlane(chunk), a.least_tiles);
-}
-
-// Inclusive sum over the lanes up to this one.
-__device__ __forceinline__ int wave_prefix(int x, int lane) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int y = __shfl_up(x, o);
-        x += lane >= o ? y : 0;
-    }
-    return x;
-}
-
-// The entry that unit u belongs to, the units before it and its own number of them; entry = -1: the launch has fewer units.
+// How the keys of the entries are divided.  Only the device knows the lengths, so every workgroup settles it for itself, all in the same way: a
+// unit has at most `chunk` tiles; chunk is the tiles of all entries over the units aimed at, raised by eighths until there are no more units than
+// workgroups were launched per head of the cache.  Long entries then get more units than short ones, and all units run at once.
 struct CacheUnit {
-    int entry, before, n;
+    CacheEntry entry;
+    int e;          // its number, -1: the launch has fewer units
+    int before, n;  // the units before the entry, and its own
 };
-__device__ __forceinline__ CacheUnit cache_find_unit(const Cache8Args& a, int u, int chunk, int lane) {
+// Units of an entry with these tiles (-1: it has no rows).  Parts are made by their number alone, so a quotient off by one in its last place does no harm.
+__device__ __forceinline__ int cache_units(int tiles, float per_chunk) { return tiles < 0 ? 0 : max((int)__builtin_ceilf((float)tiles * per_chunk), 1); }
+
+__device__ __forceinline__ CacheUnit cache_find_unit(const Cache8Args& a, int u, int lane) {
+    CacheUnit r;
+    r.e = -1;
+    auto tiles_of = [&](int e, CacheEntry* t) __attribute__((always_inline)) {
+        if (e >= a.entries) return -1;
+        *t = cache_entry(a, e);
+        return t->row0 < t->rows ? min(t->tiles, 1 << 20) : -1;
+    };
+    CacheEntry t0{};
+    const int tiles0 = tiles_of(lane, &t0);  // most launches have no more entries than lanes: then this is the only look at the lengths
+    int total = wave_total(max(tiles0, 0));
+    for (int e = 64; e < a.entries; e += 64) {
+        CacheEntry t;
+        total += wave_total(max(tiles_of(e + lane, &t), 0));
+    }
+    int chunk = max((int)(((unsigned)total + (unsigned)a.aim - 1u) / (unsigned)a.aim), a.least_tiles);
+    float per_chunk;
+    for (;;) {
+        per_chunk = 1.0f / (float)chunk;
+        int units = wave_total(cache_units(tiles0, per_chunk));
+        for (int e = 64; e < a.entries; e += 64) {
+            CacheEntry t;
+            units += wave_total(cache_units(tiles_of(e + lane, &t), per_chunk));
+        }
+        if (units <= a.limit) break;  // at the latest with one unit per entry: the limit is no less than the entries
+        chunk += (chunk + 7) >> 3;
+    }
     int before = 0;
     for (int e0 = 0; e0 < a.entries; e0 += 64) {
-        const int n = e0 + lane < a.entries ? cache_units(cache_entry(a, e0 + lane), chunk) : 0;
-        const int upto = wave_prefix(n, lane) + before;
+        CacheEntry t = t0;
+        const int n = cache_units(e0 ? tiles_of(e0 + lane, &t) : tiles0, per_chunk);
+        const int upto = wave_prefix(n) + before;
         const unsigned long long found = __ballot(u < upto);
         if (found) {
-            const int l = __builtin_amdgcn_readfirstlane(__builtin_ctzll(found));
-            const int mine = __builtin_amdgcn_readlane(n, l);
-            return {e0 + l, __builtin_amdgcn_readlane(upto, l) - mine, mine};
+            const int l = __builtin_ctzll(found);
+            r.e = e0 + l;
+            r.n = __builtin_amdgcn_readlane(n, l);
+            r.before = __builtin_amdgcn_readlane(upto, l) - r.n;
+            r.entry = cache_entry_of(a, r.e, __builtin_amdgcn_readlane(t.len, l), __builtin_amdgcn_readlane(t.q_len, l));
+            return r;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
     }
-    return {-1, 0, 0};
+    return r;
 }
-// The units before entry e, and its own.
-__device__ __forceinline__ CacheUnit cache_units_of(const Cache8Args& a, int e, int chunk, int lane) {
-    int before = 0;
-    for (int e0 = 0; e0 <= e; e0 += 64) {
-        const int n = e0 + lane < a.entries ? cache_units(cache_entry(a, e0 + lane), chunk) : 0;
-        const int upto = wave_prefix(n, lane) + before;
-        if (e < e0 + 64) {
-            const int mine = __builtin_amdgcn_readlane(n, e - e0);
-            return {e, __builtin_amdgcn_readlane(upto, e - e0) - mine, mine};
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
+
+// Tiles of part `part` of n: the first tiles % n parts have one more.  (The same for the whole wavefront, which the compiler does not see through a division.)
+__device__ __forceinline__ void cache_part(int tiles, int part, int n, int* t0, int* t1) {
+    const int share = (unsigned)tiles / (unsigned)n, more = tiles - share * n;
+    *t0 = __builtin_amdgcn_readfirstlane(part * share + min(part, more));
+    *t1 = __builtin_amdgcn_readfirstlane(*t0 + share + (part < more ? 1 : 0));
+}
+
+// What is needed of a block: its number in the pool (-1: a hole, or behind the entry's last token), how many of its tokens are there, and its scales.
+// The value's scale goes into the exponent of the probabilities, 2^(ks s + vs_log2 - m), so that a logit costs one fma and the sum of a block's
+// probabilities is put right by one more.  Where it is 0, the codes are cleared instead.
+struct CacheBlock {
+    int e, there;
+    float ks, vs_log2, vs_inv;
+};
+__device__ __forceinline__ CacheBlock cache_block(const Cache8Args& a, int kvh, int len, int blk, int page) {
+    CacheBlock x{-1, 0, 0.f, 0.f, 1.f};
+    if (kCacheBlock * blk < len && (unsigned)page < (unsigned)a.n_pages) {
+        x.e = (page * a.heads + kvh) * a.page_blocks + blk - a.by_page_blocks.quotient(blk) * a.page_blocks;
+        x.ks = a.ks[x.e] * a.scale_log2;
+        const float vs = a.vs[x.e];
+        x.there = vs == 0.f ? 0 : min(len - kCacheBlock * blk, kCacheBlock);
+        x.vs_log2 = vs == 0.f ? 0.f : __builtin_log2f(vs);
+        x.vs_inv = vs == 0.f ? 1.f : 1.0f / vs;
     }
-    return {-1, 0, 0};
+    return x;
+}
+__device__ __forceinline__ float lane_value(float x, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l)); }
+
+// The running state of a row's softmax, in both halves of the wavefront: reference maximum (log2 units), what is subtracted (0 until there is one), and the
+// sum of this half's keys.
+struct RowState {
+    float m, sub, l;
+};
+constexpr int kRescaleAbove = 8;  // log2: the reference maximum rises only when a logit is this far above it, so p stays below 2^8 and exact to rounding
+
+// Probabilities of a 32-key tile: s holds the logits of the lane's row and block.  c: the block's key scale; the result is p * vs in
+// bf16, and *sum gets the sum of the block's p.  visible: tokens of the block that the row sees (all if !EDGE).
+template <bool EDGE>
+__device__ __forceinline__ void tile_probabilities(const floatx16& s, float c, float vs_log2, float vs_inv, float sub, int visible, bf16x8* lo, bf16x8* hi, float* l) {
+    constexpr uint32_t kOnes = 0x3f803f80u;
+    const float b = vs_log2 - sub;
+    uint4v plo, phi;
+    float sum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+        float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, b)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], c, b));
+        if constexpr (EDGE) {  // chosen, not multiplied: logits of what is not seen, and scales of blocks that are not, may be no numbers
+            p0 = r < visible ? p0 : 0.f;
+            p1 = r + 1 < visible ? p1 : 0.f;
+        }
+        const uint32_t w = pack_bf16(p0, p1);
+        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, kOnes), sum, false);
+        if (r < 8) plo[r / 2] = w;
+        else phi[r / 2 - 4] = w;
+    }
+    *lo = __builtin_bit_cast(bf16x8, plo);
+    *hi = __builtin_bit_cast(bf16x8, phi);
+    if (!EDGE || visible > 0) *l = __builtin_fmaf(sum, vs_inv, *l);  // a scale that is no number is none of a row that does not see the block
 }
 
 // Eight codes as bf16, exactly: e4m3 has 4 significant bits, int8 8.
@@ -125,6 +189,8 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi) {
         const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
         return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
     } else {
+        // byte by byte in the instruction that converts (SDWA); else the compiler takes the bytes apart an iteration ahead, and 50 registers with them
+        asm("" : "+v"(lo), "+v"(hi));
         uint4v r;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

@@ -5,23 +5,28 @@
 
 namespace flat {
 
-// How many units a launch aims at: what the chip holds at once (256 compute units, two workgroups each, one at d = 256), over the heads of the
-// cache.  Which entry gets how many is settled on the device from the lengths.  With more entries than kMaxEntries nothing is divided: they fill
-// the chip by themselves, and finding one's unit would cost more than it gives.
 void cache8_plan(int B, int H, int heads, int Nq, int max_tokens, int d, Cache8Plan* out) {
-    constexpr int kMaxEntries = 1024, kLeastTiles = 8;
+    constexpr int kMaxEntries = 1024, kLeastKeys = 256;
     const long long rows = (long long)Nq * (H / heads);
-    out->rows_per_block = 32;
+    out->rows_per_block = rows <= 32 ? 32 : rows <= 64 && d != 256 ? 64 : 128;
+    out->tile_keys = out->rows_per_block > 32 ? 64 : d == 32 ? 128 : d == 64 ? 64 : 32;
     out->row_blocks = (int)((rows + out->rows_per_block - 1) / out->rows_per_block);
     const long long entries = (long long)B * out->row_blocks;
     out->entries = (int)entries;
-    out->least_tiles = kLeastTiles;
-    const long long tiles = ((long long)max_tokens + 2 * kCacheBlock - 1) / (2 * kCacheBlock);
-    const int slots = (d == 256 ? 256 : 512) / heads;
-    out->target = 0;
-    if (entries <= kMaxEntries && tiles > kLeastTiles) out->target = slots > entries ? slots : (int)entries;
-    out->max_units = (int)entries + out->target;
-    out->workspace_bytes = out->target ? (size_t)out->max_units * heads * out->rows_per_block * (d + 2) * sizeof(float) : 0;
+    out->least_tiles = kLeastKeys / out->tile_keys;
+    const long long tiles = ((long long)max_tokens + out->tile_keys - 1) / out->tile_keys;
+    // units that the chip holds at once: 256 compute units of two workgroups (d = 256: one; 64 rows of up to 64 channels: four)
+    const int slots = 256 * (d == 256 ? 1 : out->rows_per_block == 64 && d <= 64 ? 4 : 2) / heads;
+    out->aim = out->limit = 0;
+    out->parts_at = out->workspace_bytes = 0;
+    // With more entries than kMaxEntries nothing is divided: they fill the chip by themselves, and finding a unit would cost more than it gives.  Neither
+    // are blocks of many rows that fill it: their lengths differ little, and putting their many rows together costs more.
+    if (entries <= kMaxEntries && tiles > out->least_tiles && (out->rows_per_block == 32 || entries < slots)) {
+        out->aim = slots > entries ? slots : (int)entries;
+        out->limit = 2 * entries <= out->aim ? out->aim : out->aim + (int)entries;
+        out->parts_at = ((size_t)entries * 8 + 15) / 16 * 16;
+        out->workspace_bytes = out->parts_at + (size_t)out->limit * heads * out->rows_per_block * (d + 2) * sizeof(float);
+    }
 }
 
 }  // namespace flat

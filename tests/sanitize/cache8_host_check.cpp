@@ -32,8 +32,8 @@ hipError_t launch_cache8_compact(const flat_cache8&, const int*, int*, int, int,
 hipError_t launch_cache8_fwd(const flat_cache8& c, const Cache8Attend& a, const Cache8Plan& p, hipStream_t) {
     ++g_launches;
     const long long rows = (long long)a.Nq * (a.H / c.n_heads);
-    const bool fits = p.entries > 0 && (long long)a.B * p.row_blocks == p.entries && (long long)p.row_blocks * p.rows_per_block >= rows && p.max_units >= p.entries &&
-                      (long long)p.max_units * c.n_heads <= 0x7fffffffLL && (long long)a.B * c.n_heads * rows <= 0x7fffffffLL &&
+    const bool fits = p.entries > 0 && (long long)a.B * p.row_blocks == p.entries && (long long)p.row_blocks * p.rows_per_block >= rows && (p.limit == 0 || (p.limit >= p.entries && p.limit >= p.aim)) &&
+                      (long long)(p.limit ? p.limit : p.entries) * c.n_heads <= 0x7ffffff8LL && (long long)a.B * c.n_heads * rows <= 0x7fffffffLL &&
                       (long long)a.max_pages * c.page_tokens <= 0x7fffffffLL;
     return fits ? hipSuccess : hipErrorInvalidValue;
 }
