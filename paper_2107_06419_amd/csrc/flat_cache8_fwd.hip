@@ -329,32 +329,35 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     const int all_see = __builtin_amdgcn_readfirstlane(seen_by(first_row));                           // keys that every row of this wavefront sees
     const int any_sees = __builtin_amdgcn_readfirstlane(first_row < t.rows ? seen_by(last_row) : 0);  // and that some row sees: 0 without rows
 
-    const uint32_t k_lane = (4 * (col >> 3) + (col & 3)) * 16 + half * 256, v_lane = col * 16;
-    const bool k_second = (col >> 2) & 1;
+    // this wavefront's operand pairs: p = w, w + NW, ... of [K, V][sub-tile][j]; of each the lane's place in a block, and which block it is of the sub-tile
+    const uint8_t* base[MINE];
+    int sub[MINE];
+    bool second[MINE];
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) {
+        const int p = min(w + NW * x, PAIRS - 1), is_v = p >= 2 * J, q2 = p - (is_v ? 2 * J : 0);
+        sub[x] = q2 / J;
+        second[x] = is_v ? half : (col >> 2) & 1;
+        base[x] = (is_v ? a.v + col * 16 : a.k + (4 * (col >> 3) + (col & 3)) * 16 + half * 256) + 512 * (q2 - sub[x] * J);
+    }
     uint4v codes[MINE];
-    auto load = [&](int i) __attribute__((always_inline)) {  // this wavefront's share of tile i of the unit; `now` is the group it lies in
+    int now_at = 0;  // max(now.e, 0): holes read block 0, and what they read counts for nothing
+    auto load = [&](int i) __attribute__((always_inline)) {  // the share of tile i of the unit; `now` is the group it lies in
 #pragma unroll
         for (int x = 0; x < MINE; ++x) {
-            const int p = w + NW * x;
-            if (PAIRS % NW && p >= PAIRS) continue;
-            const bool is_v = p >= 2 * J;
-            const int sub = (p - (is_v ? 2 * J : 0)) / J, j = (p - (is_v ? 2 * J : 0)) % J, at = 4 * (i % GROUP) + 2 * sub;
-            const int e0 = max(__builtin_amdgcn_readlane(now.e, at), 0), e1 = max(__builtin_amdgcn_readlane(now.e, at + 1), 0);
-            const size_t at0 = (size_t)e0 * (16 * D), at1 = (size_t)e1 * (16 * D);
-            const uint8_t* base = is_v ? a.v + (half ? at1 : at0) + v_lane : a.k + (k_second ? at1 : at0) + k_lane;
-            codes[x] = *(const uint4v*)(base + 512 * j);
+            if (PAIRS % NW && w + NW * x >= PAIRS) continue;
+            const int at = 4 * (i % GROUP) + 2 * sub[x];
+            const int e0 = __builtin_amdgcn_readlane(now_at, at), e1 = __builtin_amdgcn_readlane(now_at, at + 1);
+            codes[x] = *(const uint4v*)(base[x] + (uint64_t)(uint32_t)(second[x] ? e1 : e0) * (16 * D));
         }
     };
-    auto widen = [&](int i, int buf) __attribute__((always_inline)) {  // the loaded share into LDS
+    auto widen = [&](int i, int buf, bool whole) __attribute__((always_inline)) {  // the loaded share into LDS; whole: all tokens are there
 #pragma unroll
         for (int x = 0; x < MINE; ++x) {
             const int p = w + NW * x;
             if (PAIRS % NW && p >= PAIRS) continue;
             uint4v c = codes[x];
-            if (p >= 2 * J) {
-                const int there = __builtin_bit_cast(int, scales[4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + 2 * ((p - 2 * J) / J) + half) + 3]);
-                if (__any(there < 16)) c = clear_behind(c, there);
-            }
+            if (!whole && p >= 2 * J) c = clear_behind(c, __builtin_bit_cast(int, scales[4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + 2 * sub[x] + half) + 3]));
             uint8_t* to = smem + buf * BUF + p * 2048 + lane * 16;
             *(bf16x8*)to = codes_to_bf16<FMT>(c[0], c[1]);
             *(bf16x8*)(to + 1024) = codes_to_bf16<FMT>(c[2], c[3]);
@@ -368,81 +371,125 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
         for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
     RowState st{-INFINITY, 0.f, 0.f};
 
+    // S^T of both sub-tiles, and the largest scaled logit of the row
+    auto logits = [&](const uint8_t* frag, floatx16 (&s)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 2 * J; ++j) s[b] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + (b * J * 2 + j) * 1024), q[j], s[b]);
+        }
+    };
+    auto raise = [&](float top) __attribute__((always_inline)) {
+        const float up = __builtin_fmaxf(st.m, top), to = up == -INFINITY ? 0.f : up;
+        const float by = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.sub - to);
+        st.l *= by;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[j][r] *= by;
+        st.m = up;
+        st.sub = to;
+    };
+    auto attend = [&](const uint8_t* frag, int b, const bf16x8 (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < 2 * J; ++j) o[j / 2] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + ((2 + b) * J * 2 + j) * 1024), p[j & 1], o[j / 2]);
+    };
+
     const int n = tile1 - tile0;
+    now_at = max(now.e, 0);
+    uint64_t lacking = __ballot(now.there < 16), lacking_next = 0;  // blocks of the group that `now` is, and of the one before while it is worked on
     if (n > 0) load(0);
     __syncthreads();  // the scales of the first group
     if (n > 0) {
-        widen(0, 0);
+        widen(0, 0, false);
         if (n > 1) load(1);
     }
     __syncthreads();
-    for (int i = 0; i < n; ++i) {
-        const int buf = i & 1, at = i % GROUP;
-        // what the next group's blocks are: pages at the start of this one, scales in its middle; its first tile is loaded two tiles ahead
+    // what the next group's blocks are: pages at the start of a group, scales in its middle; its first tile is loaded two tiles ahead
+    auto look_ahead = [&](int i) __attribute__((always_inline)) {
+        const int at = i % GROUP;
         if (at == 0 && i + GROUP < n) next_page = page_of(i / GROUP + 1);
-        if (at == GROUP / 2 && i + GROUP - GROUP / 2 < n) next = block_of(i / GROUP + 1, next_page);
-        if (i + 1 < n) widen(i + 1, buf ^ 1);
-        if (at == GROUP - 2) now = next;
+        if (at == GROUP / 2 && i + GROUP - GROUP / 2 < n) {
+            next = block_of(i / GROUP + 1, next_page);
+            lacking_next = __ballot(next.there < 16);
+        }
+        if (at == GROUP - 2) now_at = max(next.e, 0);
+    };
+    auto done = [&](int i) __attribute__((always_inline)) {
+        if (i % GROUP == GROUP - 1) lacking = lacking_next;
+        __syncthreads();
+    };
+    // a tile that every row sees whole, followed by one whose tokens are all there: no masks to apply
+    auto plain = [&](int i) __attribute__((always_inline)) {
+        const int at = i % GROUP;
+        const uint64_t here = (lacking >> (4 * at)) & 15, after = at == GROUP - 1 ? lacking_next & 15 : (lacking >> (4 * at + 4)) & 15;
+        return i + 2 < n && (tile0 + i) * 64 + 64 <= all_see && (here | after) == 0;
+    };
+    for (int i = 0; i < n;) {
+        look_ahead(i);
+        while (plain(i)) {
+            const int buf = i & 1;
+            const uint8_t* frag = smem + buf * BUF + lane * 16;
+            const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + half);
+            const floatx4 x0 = *(const floatx4*)sc, x1 = *(const floatx4*)(sc + 8);
+            floatx16 s[2];
+            logits(frag, s);
+            float top[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                top[b] = s[b][0];
+#pragma unroll
+                for (int r = 1; r < 16; ++r) top[b] = __builtin_fmaxf(top[b], s[b][r]);
+            }
+            const float most = halves_max(__builtin_fmaxf(top[0] * x0[0], top[1] * x1[0]));
+            // A maximum that has to rise is the other path's: with the rescaling in here, the compiler moves the accumulators to other registers and
+            // back in every tile.
+            if (__any(most > st.m + kRescaleAbove)) break;
+            bf16x8 p[2];
+            tile_probabilities<false>(s[0], x0[0], x0[1], x0[2], st.sub, 16, &p[0], &p[1], &st.l);
+            attend(frag, 0, p);
+            tile_probabilities<false>(s[1], x1[0], x1[1], x1[2], st.sub, 16, &p[0], &p[1], &st.l);
+            widen(i + 1, buf ^ 1, true);
+            load(i + 2);
+            attend(frag, 1, p);
+            done(i);
+            look_ahead(++i);
+        }
+        if (i >= n) break;
+        const int buf = i & 1, key0 = (tile0 + i) * 64;
+        if (i + 1 < n) widen(i + 1, buf ^ 1, false);
         if (i + 2 < n) load(i + 2);
-        const int key0 = (tile0 + i) * 64;
         if (key0 < any_sees) {
             const uint8_t* frag = smem + buf * BUF + lane * 16;
-            const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * at + half);
+            const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + half);
             floatx16 s[2];
+            logits(frag, s);
+            float most = -INFINITY;
+            int visible[2];
             floatx4 x[2];
-            int there[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 x[b] = *(const floatx4*)(sc + 8 * b);
                 const float last = x[b][3];  // (the bits of a vector's element taken directly would be those of its first)
-                there[b] = __builtin_bit_cast(int, last);
+                visible[b] = __builtin_bit_cast(int, last) < 0 ? 0 : min(max(seen - key0 - 32 * b - kCacheBlock * half, 0), 16);
+                float top = -INFINITY;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[b][r] = 0.f;
-#pragma unroll
-                for (int j = 0; j < 2 * J; ++j) s[b] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + (b * J * 2 + j) * 1024), q[j], s[b]);
+                for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, r < visible[b] ? s[b][r] : -INFINITY);
+                most = __builtin_fmaxf(most, top == -INFINITY ? top : top * x[b][0]);
             }
-            int visible[2];
-            float top = -INFINITY;
-            const bool edge = key0 + 64 > all_see || __any((there[0] | there[1]) < 0);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                float most = -INFINITY;
-                visible[b] = 16;
-                if (edge) {
-                    visible[b] = there[b] < 0 ? 0 : min(max(seen - key0 - 32 * b - kCacheBlock * half, 0), 16);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, r < visible[b] ? s[b][r] : -INFINITY);
-                    most = most == -INFINITY ? most : most * x[b][0];
-                } else {
-                    most = s[b][0];
-#pragma unroll
-                    for (int r = 1; r < 16; ++r) most = __builtin_fmaxf(most, s[b][r]);
-                    most *= x[b][0];
-                }
-                top = __builtin_fmaxf(top, most);
-            }
-            top = halves_max(top);
-            if (__any(top > st.m + kRescaleAbove)) {
-                const float up = __builtin_fmaxf(st.m, top), sub = up == -INFINITY ? 0.f : up;
-                const float by = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.sub - sub);
-                st.l *= by;
-#pragma unroll
-                for (int j = 0; j < J; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[j][r] *= by;
-                st.m = up;
-                st.sub = sub;
-            }
+            most = halves_max(most);
+            if (__any(most > st.m + kRescaleAbove)) raise(most);
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 bf16x8 p[2];
-                if (edge) tile_probabilities<true>(s[b], x[b][0], x[b][1], x[b][2], st.sub, visible[b], &p[0], &p[1], &st.l);
-                else tile_probabilities<false>(s[b], x[b][0], x[b][1], x[b][2], st.sub, 16, &p[0], &p[1], &st.l);
-#pragma unroll
-                for (int j = 0; j < 2 * J; ++j) o[j / 2] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + ((2 + b) * J * 2 + j) * 1024), p[j & 1], o[j / 2]);
+                tile_probabilities<true>(s[b], x[b][0], x[b][1], x[b][2], st.sub, visible[b], &p[0], &p[1], &st.l);
+                attend(frag, b, p);
             }
         }
-        __syncthreads();
+        done(i);
+        ++i;
     }
     st.l = halves_sum(st.l);
     if (a.limit && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
