@@ -3,6 +3,8 @@
 // A tile of 32 keys is S^T = K Q^T and O^T += V^T P^T on the 32 x 32 x 16 bf16 MFMAs.  Row m of the K operand is block (m / 4) % 2, token 4 (m / 8) + m % 4, so
 // that the accumulator of a lane in wave half h holds the 16 tokens of block h in order: exactly the contraction order in which the same half
 // holds V's bytes.  The probabilities go from one MFMA to the other without leaving their lane, and a lane needs the scales of one block only.
+#include <type_traits>
+
 #include "flat_cache8_fwd.hpp"
 
 namespace flat {
@@ -17,7 +19,7 @@ __device__ __forceinline__ bf16* row_of_o(const Cache8Args& a, const CacheEntry&
 }
 template <int D>
 __device__ __forceinline__ float* part_of(const Cache8Args& a, int u, int kvh) {
-    return a.parts + (size_t)(u * (size_t)a.heads + kvh) * ((size_t)a.rows_per_block * (D + 2));
+    return a.parts + (size_t)(u * (size_t)a.heads + kvh) * (32 * (D + 2));
 }
 __device__ __forceinline__ floatx2 four_bf16(const floatx4& y, float by) {
     floatx2 out;
@@ -29,47 +31,49 @@ __device__ __forceinline__ floatx2 four_bf16(const floatx4& y, float by) {
 // ---- Few rows: up to 32 of the Nq * group rows that share a head of the cache.  The four wavefronts of a workgroup take the unit's steps of
 // 32 TPS keys in turn, with K and V widened from their codes in registers: no LDS and no barrier before the end.  What bounds it is the reading of the
 // codes: a wavefront asks for the next step's as soon as this one's are widened, 8 KiB a step at d = 32 to 128, so that 64 KiB a compute unit are on their way.
-constexpr int kWaves = 4;
+constexpr int NW = 4;  // wavefronts of a workgroup, in both kernels
 
-template <int D>
-constexpr int tiles_per_step() { return D == 32 ? 4 : D == 64 ? 2 : 1; }
-
-template <int D, int FMT>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows_kernel(const Cache8Args a) {
+// DIVIDED: the entries' keys are divided over units; else a unit is an entry, and its page ids are fetched along with its lengths.
+template <int D, int FMT, bool DIVIDED>
+__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_kernel(const Cache8Args a, int lds_rows) {
     constexpr int J = D / 32;             // 16-byte pieces of a K row per wave half, and 32-channel groups of V
-    constexpr int TPS = tiles_per_step<D>(), BPS = 2 * TPS, GROUP = 64 / BPS;  // tiles and blocks of a step; steps whose blocks 64 lanes know
+    constexpr int TPS = cache8_step_keys(D) / 32, BPS = 2 * TPS, GROUP = 64 / BPS;  // tiles and blocks of a step; steps whose blocks 64 lanes know
+    constexpr int AHEAD = D == 256 ? 1 : 2;  // steps whose codes are on their way
     constexpr int RS = D + 4;             // row stride of the merge buffer, floats: spreads the rows over the banks
-    extern __shared__ __align__(16) float lds[];
+    extern __shared__ __align__(16) float lds[];  // [NW][lds_rows][RS], then statistics
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, col = lane & 31;
     const int id = blockIdx.x, u = a.by_heads.quotient(id), kvh = id - u * a.heads;
 
     CacheUnit unit;
-    if (a.limit) {
+    int step0 = 0, page0 = -1;
+    if (DIVIDED) {
         unit = cache_find_unit(a, u, lane);
         if (unit.e < 0) return;
     } else {
+        const int at = a.by_page_blocks.quotient(BPS * (w + NW * (lane / BPS)) + lane % BPS);
+        if (at < a.max_pages) page0 = a.page_table[(size_t)a.by_row_blocks.quotient(u) * a.max_pages + at];
         unit.entry = cache_entry(a, u);
         unit.e = unit.before = u;
         unit.n = 1;
     }
     const CacheEntry& t = unit.entry;
     if (t.row0 >= t.rows) return;
-    int step0, step1;
-    cache_part(t.tiles, u - unit.before, unit.n, &step0, &step1);
+    int step1 = t.tiles;
+    if (DIVIDED) cache_part(t.tiles, u - unit.before, unit.n, &step0, &step1);
 
-    // blocks of the wavefront's steps first, first + kWaves, ...
+    // blocks of the wavefront's steps first, first + NW, ...
     const int* table = a.page_table + (size_t)t.b * a.max_pages;
-    const int first = step0 + w, n_mine = first < step1 ? (step1 - first + kWaves - 1) / kWaves : 0;
-    const int my_block = BPS * (first + kWaves * (lane / BPS)) + lane % BPS;  // of this lane in the first group
+    const int first = step0 + w, n_mine = first < step1 ? (step1 - first + NW - 1) / NW : 0;
+    const int my_block = BPS * (first + NW * (lane / BPS)) + lane % BPS;  // of this lane in the first group
     auto page_of = [&](int group) __attribute__((always_inline)) {
-        const int blk = my_block + group * (BPS * kWaves * GROUP);
+        const int blk = my_block + group * (BPS * NW * GROUP);
         return kCacheBlock * blk < t.len ? table[a.by_page_blocks.quotient(blk)] : -1;
     };
     auto block_of = [&](int group, int page) __attribute__((always_inline)) {
-        return cache_block(a, kvh, t.len, my_block + group * (BPS * kWaves * GROUP), page);
+        return cache_block(a, kvh, t.len, my_block + group * (BPS * NW * GROUP), page);
     };
-    const int page0 = n_mine ? page_of(0) : -1;
+    if (DIVIDED && n_mine) page0 = page_of(0);
 
     // the rows: row = position * group + query head of the group
     const int row = t.row0 + col, pos = a.by_group.quotient(row);
@@ -88,21 +92,20 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
 
     CacheBlock now = block_of(0, page0), next = now;
     int next_page = -1;
-    int now_e = now.e;
-    const uint32_t k_lane = (4 * (col >> 3) + (col & 3)) * 16 + half * 256, v_lane = col * 16;
-    const bool k_second = (col >> 2) & 1;
-    uint4v kc[TPS][J], vc[TPS][J];
-    auto load = [&](const uint8_t* pool, int e, int at, uint32_t mine, bool second, uint4v (&x)[TPS][J]) __attribute__((always_inline)) {
+    int now_at = max(now.e, 0);  // of the group that the next loads are for; holes read block 0, and what they read counts for nothing
+    uint64_t lacking = __ballot(now.there < 16);  // blocks of the group of which a token or more is not there
+    const uint8_t *k_lane = a.k + (4 * (col >> 3) + (col & 3)) * 16 + half * 256, *v_lane = a.v + col * 16;
+    uint4v kc[AHEAD][TPS][J], vc[AHEAD][TPS][J];
+    auto load = [&](const uint8_t* mine, int e, int at, int second, uint4v (&x)[TPS][J]) __attribute__((always_inline)) {
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
-            const int e0 = max(__builtin_amdgcn_readlane(e, BPS * at + 2 * t2), 0), e1 = max(__builtin_amdgcn_readlane(e, BPS * at + 2 * t2 + 1), 0);
-            const uint8_t* p = pool + (second ? (size_t)e1 * (16 * D) : (size_t)e0 * (16 * D)) + mine;
+            const uint8_t* p = mine + (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * (BPS * at + 2 * t2 + second), e) * (16 * D);
 #pragma unroll
             for (int j = 0; j < J; ++j) x[t2][j] = *(const uint4v*)(p + 512 * j);
         }
     };
-    auto load_k = [&](int at) __attribute__((always_inline)) { load(a.k, now_e, at, k_lane, k_second, kc); };
-    auto load_v = [&](int at) __attribute__((always_inline)) { load(a.v, now_e, at, v_lane, half, vc); };
+    auto load_k = [&](int i, int set) __attribute__((always_inline)) { load(k_lane, now_at, i % GROUP, (col >> 2) & 1, kc[set]); };
+    auto load_v = [&](int i, int set) __attribute__((always_inline)) { load(v_lane, now_at, i % GROUP, half, vc[set]); };
 
     floatx16 o[J];
 #pragma unroll
@@ -111,38 +114,45 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
         for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
     RowState st{-INFINITY, 0.f, 0.f};
 
-    if (n_mine > 0) {
-        load_k(0);
-        load_v(0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        if (i < n_mine) {
+            load_k(i, i);
+            load_v(i, i);
+        }
     }
-    for (int i = 0; i < n_mine; ++i) {
+    auto step = [&](int i, auto which) __attribute__((always_inline)) {
+        constexpr int SET = decltype(which)::value;
         const int at = i % GROUP;
         // pages and scales of the next GROUP steps: fetched over these, so that their two round trips are not waited for
         if (at == 0 && i + GROUP < n_mine) next_page = page_of(i / GROUP + 1);
         if (at == GROUP / 2 && i + GROUP - GROUP / 2 < n_mine) next = block_of(i / GROUP + 1, next_page);
         float c[TPS], vs_log2[TPS], vs_inv[TPS];
-        int there[TPS], lack = 0;
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
-            const int s0 = BPS * at + 2 * t2, s1 = s0 + 1;
-            const int n0 = __builtin_amdgcn_readlane(now.there, s0), n1 = __builtin_amdgcn_readlane(now.there, s1);
-            lack |= (16 - n0) | (16 - n1);
-            there[t2] = half ? n1 : n0;
-            c[t2] = half ? lane_value(now.ks, s1) : lane_value(now.ks, s0);
-            vs_log2[t2] = half ? lane_value(now.vs_log2, s1) : lane_value(now.vs_log2, s0);
-            vs_inv[t2] = half ? lane_value(now.vs_inv, s1) : lane_value(now.vs_inv, s0);
+            const int from = 4 * (BPS * at + 2 * t2 + half);
+            c[t2] = value_of_lane(from, now.ks);
+            vs_log2[t2] = value_of_lane(from, now.vs_log2);
+            vs_inv[t2] = value_of_lane(from, now.vs_inv);
         }
-        int hole[TPS];
+        const int key0 = (first + NW * i) * (32 * TPS);
+        const bool edge = key0 + 32 * TPS > all_see || ((lacking >> (BPS * at)) & ((1ull << BPS) - 1)) != 0;
+        int there[TPS], hole[TPS];
+        if (edge) {
 #pragma unroll
-        for (int t2 = 0; t2 < TPS; ++t2) hole[t2] = half ? __builtin_amdgcn_readlane(now.e, BPS * at + 2 * t2 + 1) : __builtin_amdgcn_readlane(now.e, BPS * at + 2 * t2);
+            for (int t2 = 0; t2 < TPS; ++t2) {
+                const int from = 4 * (BPS * at + 2 * t2 + half);
+                there[t2] = __builtin_amdgcn_ds_bpermute(from, now.there);
+                hole[t2] = __builtin_amdgcn_ds_bpermute(from, now.e);
+            }
+        }
         if (at == GROUP - 1) {
             now = next;
-            now_e = now.e;
+            lacking = __ballot(now.there < 16);
         }
+        if (at == GROUP - AHEAD) now_at = max(next.e, 0);
 
         floatx16 s[TPS];
-        const int key0 = (first + kWaves * i) * (32 * TPS);
-        const bool edge = key0 + 32 * TPS > all_see || lack != 0;
         int visible[TPS];
         float top = -INFINITY;
 #pragma unroll
@@ -151,13 +161,13 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
             for (int r = 0; r < 16; ++r) s[t2][r] = 0.f;
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[t2][j][0], kc[t2][j][1]), q[2 * j], s[t2]);
-                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[t2][j][2], kc[t2][j][3]), q[2 * j + 1], s[t2]);
+                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[SET][t2][j][0], kc[SET][t2][j][1]), q[2 * j], s[t2]);
+                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[SET][t2][j][2], kc[SET][t2][j][3]), q[2 * j + 1], s[t2]);
                 if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);  // the widening takes registers: not all of it at once
             }
         }
-        // K's registers are free: the next step's codes into them, and V's below
-        if (i + 1 < n_mine) load_k((i + 1) % GROUP);
+        // K's registers are free: the codes of the step after next into them, and V's below
+        if (i + AHEAD < n_mine) load_k(i + AHEAD, SET);
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
             visible[t2] = 16;
@@ -165,7 +175,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
             if (edge) {
                 visible[t2] = hole[t2] < 0 ? 0 : min(max(seen - key0 - 32 * t2 - kCacheBlock * half, 0), 16);
 #pragma unroll
-                for (int j = 0; j < J; ++j) vc[t2][j] = clear_behind(vc[t2][j], there[t2]);
+                for (int j = 0; j < J; ++j) vc[SET][t2][j] = clear_behind(vc[SET][t2][j], there[t2]);
                 most = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, r < visible[t2] ? s[t2][r] : -INFINITY);
@@ -197,17 +207,22 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
             else tile_probabilities<false>(s[t2], c[t2], vs_log2[t2], vs_inv[t2], st.sub, 16, &lo, &hi, &st.l);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[t2][j][0], vc[t2][j][1]), lo, o[j]);
-                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[t2][j][2], vc[t2][j][3]), hi, o[j]);
+                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[SET][t2][j][0], vc[SET][t2][j][1]), lo, o[j]);
+                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[SET][t2][j][2], vc[SET][t2][j][3]), hi, o[j]);
                 if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (i + 1 < n_mine) load_v((i + 1) % GROUP);
+        if (i + AHEAD < n_mine) load_v(i + AHEAD, SET);
+    };
+    for (int i = 0; i < n_mine;) {
+        step(i, std::integral_constant<int, 0>());
+        if (AHEAD > 1 && ++i < n_mine) step(i, std::integral_constant<int, AHEAD - 1>());
+        ++i;
     }
     st.l = halves_sum(st.l);
 
-    // the four wavefronts' parts: every one scales its own to the common maximum, then all add up
-    float* stat = lds + kWaves * 32 * RS;  // [kWaves][2][32]
+    // the wavefronts' parts: every one scales its own to the common maximum, then all add up
+    float* stat = lds + NW * lds_rows * RS;  // [NW][2][32]
     if (half == 0) {
         stat[w * 64 + col] = st.m;
         stat[w * 64 + 32 + col] = st.l;
@@ -216,10 +231,10 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
     auto joined = [&](int r, float* top, float* sum) __attribute__((always_inline)) {
         float m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) m = __builtin_fmaxf(m, stat[i * 64 + r]);
+        for (int i = 0; i < NW; ++i) m = __builtin_fmaxf(m, stat[i * 64 + r]);
         float l = 0.f;
 #pragma unroll
-        for (int i = 0; i < kWaves; ++i) {
+        for (int i = 0; i < NW; ++i) {
             const float mi = stat[i * 64 + r], li = stat[i * 64 + 32 + r];
             l += mi == -INFINITY ? li : li * __builtin_amdgcn_exp2f(mi - m);  // without a maximum the sum is 0, or not a number
         }
@@ -238,18 +253,18 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
                 floatx4 y;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) y[r] = o[j][4 * x + r] * mine;
-                *(floatx4*)(lds + (w * 32 + col) * RS + 32 * j + 8 * x + 4 * half) = y;
+                *(floatx4*)(lds + (w * lds_rows + col) * RS + 32 * j + 8 * x + 4 * half) = y;
             }
     }
     __syncthreads();
     constexpr int Q4 = D / 4;  // 16-byte groups of columns per row
     float* part = part_of<D>(a, u, kvh);
-    for (int x = tid; x < rows * Q4; x += 64 * kWaves) {
+    for (int x = tid; x < rows * Q4; x += 64 * NW) {
         const int r = x / Q4, c4 = x - r * Q4;
         floatx4 y = *(const floatx4*)(lds + r * RS + 4 * c4);
 #pragma unroll
-        for (int i = 1; i < kWaves; ++i) y += *(const floatx4*)(lds + (i * 32 + r) * RS + 4 * c4);
-        if (unit.n > 1) {
+        for (int i = 1; i < NW; ++i) y += *(const floatx4*)(lds + (i * lds_rows + r) * RS + 4 * c4);
+        if (DIVIDED && unit.n > 1) {
             *(floatx4*)(part + r * D + 4 * c4) = y;
             continue;
         }
@@ -257,17 +272,17 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 1 : 2) void cache8_few_rows
         joined(r, &m, &l);
         *(floatx2*)(row_of_o<D>(a, t, kvh, t.row0 + r) + 4 * c4) = four_bf16(y, l == 0.f ? 0.f : 1.0f / l);
     }
-    if (unit.n > 1 && tid < rows) {
+    if (DIVIDED && unit.n > 1 && tid < rows) {
         part[32 * D + tid] = top;
         part[32 * D + 32 + tid] = sum;
     }
-    if (a.limit && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
+    if (DIVIDED && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
 }
 
-// ---- More rows: every wavefront has 32 rows of its own and takes all keys of the unit.  The workgroup widens each tile of 64 keys once, in
+// ---- Many rows: every wavefront has 32 rows of its own and takes all keys of the entry.  The workgroup widens each tile of 64 keys once, in
 // LDS, as the MFMA operands in the order of their lanes (1 KiB each), so that reading and writing them meets no bank twice; while a tile is
 // worked on, the next one's codes are widened and the loads of the one after it are in flight.  One barrier per tile.
-template <int D, int FMT, int NW>
+template <int D, int FMT>
 __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(const Cache8Args a, int blocks_per_xcd) {
     constexpr int J = D / 32, PAIRS = 4 * J;            // pairs of operands of a tile: K of (sub-tile, j), then V
     constexpr int MINE = (PAIRS + NW - 1) / NW;         // of a wavefront: pairs w, w + NW, ...
@@ -277,36 +292,20 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     float* scales = (float*)(smem + 2 * BUF);           // [2][64 blocks][4]: ks, vs_log2, vs_inv, tokens there as int (-1: a hole)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, col = lane & 31;
-    // units of one batch entry and head follow each other on one XCD: they read the same codes
-    const int id = xcd_logical_block(blockIdx.x, blocks_per_xcd);
-    int u, kvh;
-    CacheUnit unit;
-    if (a.limit) {
-        u = a.by_heads.quotient(id);
-        kvh = id - u * a.heads;
-        unit = cache_find_unit(a, u, lane);
-        if (unit.e < 0) return;
-    } else {
-        const int bh = a.by_row_blocks.quotient(id), b = a.by_heads.quotient(bh);
-        if (b >= a.B) return;
-        kvh = bh - b * a.heads;
-        u = b * a.row_blocks + a.row_blocks - 1 - (id - bh * a.row_blocks);  // later rows see more keys: they go first
-        unit.entry = cache_entry(a, u);
-        unit.e = unit.before = u;
-        unit.n = 1;
-    }
-    const CacheEntry& t = unit.entry;
+    // blocks of one batch entry and head follow each other on one XCD: they read the same codes.  Later rows see more keys: they go first
+    const int id = xcd_logical_block(blockIdx.x, blocks_per_xcd), bh = a.by_row_blocks.quotient(id), b = a.by_heads.quotient(bh), kvh = bh - b * a.heads;
+    if (b >= a.B) return;
+    const CacheEntry t = cache_entry(a, b * a.row_blocks + a.row_blocks - 1 - (id - bh * a.row_blocks));
     if (t.row0 >= t.rows) return;
-    int tile0, tile1;
-    cache_part(t.tiles, u - unit.before, unit.n, &tile0, &tile1);
+    const int n = t.tiles;
 
     const int* table = a.page_table + (size_t)t.b * a.max_pages;
     auto page_of = [&](int group) __attribute__((always_inline)) {
-        const int blk = 4 * (tile0 + GROUP * group) + lane;
+        const int blk = 4 * GROUP * group + lane;
         return kCacheBlock * blk < t.len ? table[a.by_page_blocks.quotient(blk)] : -1;
     };
     auto block_of = [&](int group, int page) __attribute__((always_inline)) {
-        const CacheBlock x = cache_block(a, kvh, t.len, 4 * (tile0 + GROUP * group) + lane, page);
+        const CacheBlock x = cache_block(a, kvh, t.len, 4 * GROUP * group + lane, page);
         if (w == 0) *(floatx4*)(scales + 4 * (64 * (group & 1) + lane)) = floatx4{x.ks, x.vs_log2, x.vs_inv, __builtin_bit_cast(float, x.e < 0 ? -1 : x.there)};
         return x;
     };
@@ -397,7 +396,6 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
         for (int j = 0; j < 2 * J; ++j) o[j / 2] = mfma_bf16_32x32x16(*(const bf16x8*)(frag + ((2 + b) * J * 2 + j) * 1024), p[j & 1], o[j / 2]);
     };
 
-    const int n = tile1 - tile0;
     now_at = max(now.e, 0);
     uint64_t lacking = __ballot(now.there < 16), lacking_next = 0;  // blocks of the group that `now` is, and of the one before while it is worked on
     if (n > 0) load(0);
@@ -425,7 +423,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     auto plain = [&](int i) __attribute__((always_inline)) {
         const int at = i % GROUP;
         const uint64_t here = (lacking >> (4 * at)) & 15, after = at == GROUP - 1 ? lacking_next & 15 : (lacking >> (4 * at + 4)) & 15;
-        return i + 2 < n && (tile0 + i) * 64 + 64 <= all_see && (here | after) == 0;
+        return i + 2 < n && 64 * i + 64 <= all_see && (here | after) == 0;
     };
     for (int i = 0; i < n;) {
         look_ahead(i);
@@ -458,7 +456,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
             look_ahead(++i);
         }
         if (i >= n) break;
-        const int buf = i & 1, key0 = (tile0 + i) * 64;
+        const int buf = i & 1, key0 = 64 * i;
         if (i + 1 < n) widen(i + 1, buf ^ 1, false);
         if (i + 2 < n) load(i + 2);
         if (key0 < any_sees) {
@@ -492,49 +490,95 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
         ++i;
     }
     st.l = halves_sum(st.l);
-    if (a.limit && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
     if (!has_row) return;
-    if (unit.n == 1) {
-        const float by = st.l == 0.f ? 0.f : 1.0f / st.l;
-        bf16* to = row_of_o<D>(a, t, kvh, row) + 4 * half;
+    const float by = st.l == 0.f ? 0.f : 1.0f / st.l;
+    bf16* to = row_of_o<D>(a, t, kvh, row) + 4 * half;
 #pragma unroll
-        for (int j = 0; j < J; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) *(floatx2*)(to + 32 * j + 8 * x) = four_bf16(floatx4{o[j][4 * x], o[j][4 * x + 1], o[j][4 * x + 2], o[j][4 * x + 3]}, by);
-    } else {
-        float *part = part_of<D>(a, u, kvh), *to = part + (32 * w + col) * D + 4 * half, *stat = part + 32 * NW * D + 32 * w + col;
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) *(floatx4*)(to + 32 * j + 8 * x) = floatx4{o[j][4 * x], o[j][4 * x + 1], o[j][4 * x + 2], o[j][4 * x + 3]};
-        if (half == 0) {
-            stat[0] = st.m;
-            stat[32 * NW] = st.l;
-        }
-    }
+        for (int x = 0; x < 4; ++x) *(floatx2*)(to + 32 * j + 8 * x) = four_bf16(floatx4{o[j][4 * x], o[j][4 * x + 1], o[j][4 * x + 2], o[j][4 * x + 3]}, by);
 }
 
-// ---- Puts the parts of a row together whose entry was divided: THREADS threads per row and COLS columns.  M = max m_s, O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.
-// A chain of round trips (the entry's units, then statistics and results together), so the first results are fetched before their weights are known.
-template <int D, int THREADS, int COLS>
-__global__ __launch_bounds__(THREADS) void cache8_merge_kernel(const Cache8Args a, const Divisor by_rows, int rows_per_b) {
-    constexpr int Q4 = COLS / 4, LANES = THREADS / Q4, WAVES = THREADS / 64, AHEAD = 4;
+// ---- Puts the parts of a row together whose entry was divided.  M = max m_s, O = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s.  Both kernels are chains of
+// round trips (the entry's units, then statistics and results together), so the first results are asked for before their weights are known.
+__device__ __forceinline__ float part_weight(float m, float l, float top) {
+    return m == -INFINITY ? (l == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m - top);  // no key seen: nothing; what is no number stays so
+}
+__device__ __forceinline__ void add_part(floatx4& acc, float wt, const floatx4& y) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] = wt == 0.f ? acc[i] : acc[i] + wt * y[i];
+}
+
+// Few parts per entry: a wavefront per row.  Workgroups whose entry was not divided end at once.
+template <int D>
+__global__ __launch_bounds__(256) void cache8_merge_kernel(const Cache8Args a) {
+    constexpr int Q4 = D / 4, LANES = 64 / Q4, AHEAD = 8;
+    const int lane = threadIdx.x & 63;
+    const int e = a.by_heads.quotient(blockIdx.x), kvh = blockIdx.x - e * a.heads;
+    const int2 unit = a.units[e];  // unset where the entry has no rows
+    const CacheEntry t = cache_entry(a, e);
+    const int r = 4 * blockIdx.y + (threadIdx.x >> 6), row = t.row0 + r;
+    if (row >= t.rows || unit.y == 1) return;
+    const int n = unit.y, c4 = lane % Q4, first = lane / Q4 < LANES ? lane / Q4 : n;  // d = 96: some lanes have no column
+    const size_t size = 32 * (D + 2), stride = size * a.heads;
+    const float* base = a.parts + ((size_t)unit.x * a.heads + kvh) * size;
+    const float *m_of = base + 32 * D + r, *o_of = base + (size_t)r * D + 4 * c4;
+    floatx4 ahead[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+        ahead[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (first + i * LANES < n) ahead[i] = *(const floatx4*)(o_of + (size_t)(first + i * LANES) * stride);
+    }
+    float top = -INFINITY;
+    for (int s = lane; s < n; s += 64) top = __builtin_fmaxf(top, m_of[s * stride]);
+    top = wave_max(top);
+    floatx4 acc{0.f, 0.f, 0.f, 0.f};
+    float L = 0.f;
+    for (int s0 = 0; s0 < n; s0 += 64) {
+        float wt = 0.f;
+        if (s0 + lane < n) {
+            const float m = m_of[(s0 + lane) * stride], l = m_of[(s0 + lane) * stride + 32];
+            wt = part_weight(m, l, top);
+            L += wt * l;
+        }
+        const int end = min(n - s0, 64);
+        if (s0 == 0) {
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) add_part(acc, __shfl(wt, min(first + i * LANES, 63)), ahead[i]);  // those behind n have weight 0, or fetched nothing
+        }
+        for (int i = s0 ? 0 : AHEAD * LANES; i < end; i += LANES) {
+            const float x = __shfl(wt, min(first + i, 63));
+            if (first + i < end) add_part(acc, x, *(const floatx4*)(o_of + (size_t)(s0 + first + i) * stride));
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o);
+    floatx4 all = acc;
+#pragma unroll
+    for (int k = 1; k < LANES; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) all[i] += __shfl(acc[i], min(k * Q4 + c4, 63));
+    if (lane < Q4) *(floatx2*)(row_of_o<D>(a, t, kvh, row) + 4 * c4) = four_bf16(all, L == 0.f ? 0.f : 1.0f / L);
+}
+
+// Many parts per entry: a workgroup per row and 32 columns.
+template <int D>
+__global__ __launch_bounds__(256) void cache8_merge_many_kernel(const Cache8Args a) {
+    constexpr int THREADS = 256, COLS = 32, Q4 = COLS / 4, LANES = THREADS / Q4, WAVES = THREADS / 64, AHEAD = 4;
     __shared__ floatx4 red[THREADS];
     __shared__ float wts[THREADS], stat[2][WAVES];
     const int tid = threadIdx.x, lane = tid & 63;
-    // blockIdx.x = (b * heads + head of the cache) * rows_per_b + row
-    const int bh = by_rows.quotient(blockIdx.x), row = blockIdx.x - bh * rows_per_b;
-    const int b = a.by_heads.quotient(bh), kvh = bh - b * a.heads;
-    const int rb = row / a.rows_per_block, e = b * a.row_blocks + rb, r = row - a.rows_per_block * rb;
-    const int2 unit = a.units[e];  // unset where the entry has no rows
-    const int q_len = a.q_lens ? min(max(a.q_lens[b], 0), a.Nq) : a.Nq;
-    if (row >= q_len * a.group || unit.y == 1) return;
+    const int e = a.by_heads.quotient(blockIdx.x), kvh = blockIdx.x - e * a.heads;
+    const int2 unit = a.units[e];
+    const CacheEntry t = cache_entry(a, e);
+    const int r = blockIdx.y, row = t.row0 + r;
+    if (row >= t.rows || unit.y == 1) return;
     const int n = unit.y;
-    const size_t size = (size_t)a.rows_per_block * (D + 2), stride = size * a.heads;
+    const size_t size = 32 * (D + 2), stride = size * a.heads;
     const float* base = a.parts + ((size_t)unit.x * a.heads + kvh) * size;
-    const float* m_of = base + (size_t)a.rows_per_block * D + r;
-    const int c4 = tid % Q4, first = tid / Q4 < LANES ? tid / Q4 : n;  // d = 96: some threads have no column
-    const float* o_of = base + (size_t)r * D + COLS * blockIdx.y + 4 * c4;
+    const float* m_of = base + 32 * D + r;
+    const int c4 = tid % Q4, first = tid / Q4;
+    const float* o_of = base + (size_t)r * D + COLS * blockIdx.z + 4 * c4;
 
     floatx4 ahead[AHEAD];
 #pragma unroll
@@ -545,45 +589,38 @@ __global__ __launch_bounds__(THREADS) void cache8_merge_kernel(const Cache8Args 
     float top = -INFINITY, m0 = -INFINITY, l0 = 0.f;
     if (tid < n) {
         m0 = m_of[tid * stride];
-        l0 = m_of[tid * stride + a.rows_per_block];
+        l0 = m_of[tid * stride + 32];
     }
     top = m0;
     for (int s = tid + THREADS; s < n; s += THREADS) top = __builtin_fmaxf(top, m_of[s * stride]);
     top = wave_max(top);
-    if (WAVES > 1) {
-        if (lane == 0) stat[0][tid >> 6] = top;
-        __syncthreads();
+    if (lane == 0) stat[0][tid >> 6] = top;
+    __syncthreads();
 #pragma unroll
-        for (int i = 0; i < WAVES; ++i) top = __builtin_fmaxf(top, stat[0][i]);
-    }
+    for (int i = 0; i < WAVES; ++i) top = __builtin_fmaxf(top, stat[0][i]);
     floatx4 acc{0.f, 0.f, 0.f, 0.f};
     float L = 0.f;
     for (int s0 = 0; s0 < n; s0 += THREADS) {
         if (s0 + tid < n) {
             if (s0) {
                 m0 = m_of[(s0 + tid) * stride];
-                l0 = m_of[(s0 + tid) * stride + a.rows_per_block];
+                l0 = m_of[(s0 + tid) * stride + 32];
             }
-            const float wt = m0 == -INFINITY ? (l0 == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(m0 - top);  // no key seen: nothing; what is no number stays so
+            const float wt = part_weight(m0, l0, top);
             wts[tid] = wt;
             L += wt * l0;
         }
         __syncthreads();
-        auto add = [&](int s, const floatx4& y) __attribute__((always_inline)) {
-            const float wt = wts[s];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[i] = wt == 0.f ? acc[i] : acc[i] + wt * y[i];
-        };
         const int end = min(n - s0, THREADS);
         int s = first;
         if (s0 == 0) {
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i)
-                if (first + i * LANES < end) add(first + i * LANES, ahead[i]);
+                if (first + i * LANES < end) add_part(acc, wts[first + i * LANES], ahead[i]);
             s = first + AHEAD * LANES;
         }
 #pragma unroll 4
-        for (; s < end; s += LANES) add(s, *(const floatx4*)(o_of + (size_t)(s0 + s) * stride));
+        for (; s < end; s += LANES) add_part(acc, wts[s], *(const floatx4*)(o_of + (size_t)(s0 + s) * stride));
         __syncthreads();
     }
 #pragma unroll
@@ -592,58 +629,50 @@ __global__ __launch_bounds__(THREADS) void cache8_merge_kernel(const Cache8Args 
     red[tid] = acc;
     __syncthreads();
     if (tid >= Q4) return;
-    L = 0.f;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) L += stat[1][i];
+    L = (stat[1][0] + stat[1][1]) + (stat[1][2] + stat[1][3]);
     for (int k = 1; k < LANES; ++k) acc += red[k * Q4 + c4];
-    const int p = a.by_group.quotient(row), g = row - p * a.group;
-    *(floatx2*)(a.O + ((size_t)(b * (size_t)a.H + kvh * a.group + g) * a.Nq + p) * D + COLS * blockIdx.y + 4 * c4) = four_bf16(acc, L == 0.f ? 0.f : 1.0f / L);
+    *(floatx2*)(row_of_o<D>(a, t, kvh, row) + COLS * blockIdx.z + 4 * c4) = four_bf16(acc, L == 0.f ? 0.f : 1.0f / L);
 }
 
-template <int D, int FMT>
+template <int D, int FMT, bool DIVIDED>
 hipError_t launch_few(const Cache8Args& args, hipStream_t stream) {
     static std::atomic<uint64_t> lds_allowed{0};
-    constexpr int lds = (kWaves * 32 * (D + 4) + kWaves * 64) * (int)sizeof(float);
-    const hipError_t e = allow_dynamic_lds((const void*)cache8_few_rows_kernel<D, FMT>, lds, &lds_allowed);
+    constexpr auto lds_bytes = [](int rows) { return (NW * rows * (D + 4) + NW * 64) * (int)sizeof(float); };
+    static_assert(lds_bytes(32) <= 160 * 1024, "the wavefronts' results must fit the LDS");
+    const hipError_t e = allow_dynamic_lds((const void*)cache8_few_rows_kernel<D, FMT, DIVIDED>, lds_bytes(32), &lds_allowed);
     if (e != hipSuccess) return e;
-    const unsigned units = (unsigned)(args.limit ? args.limit : args.entries);
-    hipLaunchKernelGGL((cache8_few_rows_kernel<D, FMT>), dim3(units * (unsigned)args.heads), dim3(64 * kWaves), lds, stream, args);
+    const int rows = args.Nq * args.group < 32 ? args.Nq * args.group : 32;
+    const unsigned units = (unsigned)(DIVIDED ? args.limit : args.entries);
+    hipLaunchKernelGGL((cache8_few_rows_kernel<D, FMT, DIVIDED>), dim3(units * (unsigned)args.heads), dim3(64 * NW), lds_bytes(rows), stream, args, rows);
     return hipGetLastError();
 }
 
-template <int D, int FMT, int NW>
+template <int D, int FMT>
 hipError_t launch_rows(const Cache8Args& args, hipStream_t stream) {
     static std::atomic<uint64_t> lds_allowed{0};
     constexpr int lds = 2 * (D / 32) * 4 * 2048 + 2 * 64 * 16;
-    const hipError_t e = allow_dynamic_lds((const void*)cache8_rows_kernel<D, FMT, NW>, lds, &lds_allowed);
+    const hipError_t e = allow_dynamic_lds((const void*)cache8_rows_kernel<D, FMT>, lds, &lds_allowed);
     if (e != hipSuccess) return e;
-    const int per_xcd = (int)(((long long)(args.limit ? args.limit : args.entries) * args.heads + 7) / 8);
-    hipLaunchKernelGGL((cache8_rows_kernel<D, FMT, NW>), dim3((unsigned)per_xcd * 8u), dim3(64 * NW), lds, stream, args, per_xcd);
+    const int per_xcd = (int)(((long long)args.entries * args.heads + 7) / 8);
+    hipLaunchKernelGGL((cache8_rows_kernel<D, FMT>), dim3((unsigned)per_xcd * 8u), dim3(64 * NW), lds, stream, args, per_xcd);
     return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_merge(const Cache8Args& args, hipStream_t stream) {
-    const int rows = args.Nq * args.group;
-    const unsigned grid = (unsigned)(args.B * args.heads) * (unsigned)rows;
-    if (args.limit <= 4 * args.entries) hipLaunchKernelGGL((cache8_merge_kernel<D, 64, D>), dim3(grid), dim3(64), 0, stream, args, Divisor(rows), rows);
-    else hipLaunchKernelGGL((cache8_merge_kernel<D, 256, 32>), dim3(grid, D / 32), dim3(256), 0, stream, args, Divisor(rows), rows);
+    const int rows = args.Nq * args.group < 32 ? args.Nq * args.group : 32;  // that a block has at most
+    const unsigned grid = (unsigned)args.entries * (unsigned)args.heads;
+    if (args.limit <= 16 * args.entries) hipLaunchKernelGGL((cache8_merge_kernel<D>), dim3(grid, (unsigned)(rows + 3) / 4), dim3(256), 0, stream, args);
+    else hipLaunchKernelGGL((cache8_merge_many_kernel<D>), dim3(grid, (unsigned)rows, D / 32), dim3(256), 0, stream, args);
     return hipGetLastError();
 }
 
 template <int D, int FMT>
 hipError_t launch(const Cache8Args& args, hipStream_t stream) {
     hipError_t e;
-    switch (args.rows_per_block) {
-        case 32: e = launch_few<D, FMT>(args, stream); break;
-        case 64:
-            if constexpr (D != 256) {  // (two wavefronts would have 16 operand pairs of a tile each on their way: too many registers)
-                e = launch_rows<D, FMT, 2>(args, stream);
-                break;
-            }
-            [[fallthrough]];
-        default: e = launch_rows<D, FMT, 4>(args, stream); break;
-    }
+    if (args.rows_per_block > 32) e = launch_rows<D, FMT>(args, stream);
+    else if (args.limit) e = launch_few<D, FMT, true>(args, stream);
+    else e = launch_few<D, FMT, false>(args, stream);
     return e != hipSuccess || args.limit == 0 ? e : launch_merge<D>(args, stream);
 }
 

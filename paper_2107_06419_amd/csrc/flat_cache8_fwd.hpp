@@ -147,7 +147,8 @@ __device__ __forceinline__ CacheBlock cache_block(const Cache8Args& a, int kvh, 
     }
     return x;
 }
-__device__ __forceinline__ float lane_value(float x, int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), l)); }
+// x of lane (byte address / 4).
+__device__ __forceinline__ float value_of_lane(int at, float x) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(at, __builtin_bit_cast(int, x))); }
 
 // The running state of a row's softmax, in both halves of the wavefront: reference maximum (log2 units), what is subtracted (0 until there is one), and the
 // sum of this half's keys.

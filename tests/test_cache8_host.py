@@ -85,8 +85,9 @@ def test_attend_workspace_sizes():
     assert size(0, 4, 2, 1, 100, 64) == 0 and size(1, 3, 2, 1, 100, 64) == 0 and size(1, 4, 2, 1, 100, 48) == 0 and size(1, 4, 2, 1, 0, 64) == 0
     assert size(1, 4, 2, 1, 64, 64) == 0                                      # a cache of a few tiles is not divided
     assert size(1, 1, 1, 1, 1 << 30, 128) == size(1, 1, 1, 1, 1 << 20, 128)   # the size does not grow with the cache
-    for B, H, heads, Nq, d in ((1, 16, 16, 1, 64), (64, 64, 8, 1, 128), (3, 5, 1, 7, 256), (200, 8, 8, 4, 96)):
+    for B, H, heads, Nq, d in ((1, 16, 16, 1, 64), (4, 64, 8, 1, 128), (3, 5, 1, 7, 256), (20, 8, 8, 4, 96)):
         assert 0 < size(B, H, heads, Nq, 1 << 17, d) < 1 << 28
+    assert size(64, 64, 8, 1, 1 << 17, 128) == 0 and size(2, 16, 16, 4096, 1 << 14, 128) == 0   # entries that fill the chip are not divided either
 
 
 def test_page_calls_refuse():
