@@ -52,16 +52,6 @@ __device__ __forceinline__ CacheEntry cache_entry(const Cache8Args& a, int e) {
     return cache_entry_of(a, e, len, q_len);
 }
 
-// Inclusive sums over the lanes of a wavefront: within rows of 16 lanes, then the rows' totals carried on.
-__device__ __forceinline__ int wave_prefix(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // from the lane 1, 2, 4, 8 before, in the row
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next one (rows 1 and 3)
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
-    return x;
-}
 __device__ __forceinline__ int wave_total(int x) { return __builtin_amdgcn_readlane(wave_prefix(x), 63); }
 
 // How the keys of the entries are divided.  Only the device knows the lengths, so every workgroup settles it for itself, all in the same way: a

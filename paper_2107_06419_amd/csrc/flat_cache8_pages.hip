@@ -100,18 +100,31 @@ __global__ __launch_bounds__(kThreads) void cache8_fork_kernel(const PageArgs a,
 constexpr int kListThreads = 1024;
 constexpr int kListWaves = kListThreads / 64;
 
-__device__ __forceinline__ void mark_held(uint32_t* bits, int n_pages, const int* table, long long n) {
+// One compute unit reads the whole table, so what bounds it is how much is on its way: 16 bytes a load, eight loads a thread, 128 KiB at once.
+__device__ __forceinline__ void mark_held(uint32_t* bits, int n_pages, const int* table, int n) {
     const int tid = threadIdx.x;
+    auto mark = [&](int id) __attribute__((always_inline)) {
+        if ((unsigned)id < (unsigned)n_pages) atomicOr(&bits[id >> 5], 1u << (id & 31));
+    };
     for (int i = tid; i < (n_pages + 63) / 64 * 2; i += kListThreads) bits[i] = 0;
     __syncthreads();
+    const int head = min((int)((0 - (reinterpret_cast<uintptr_t>(table) >> 2)) & 3), n);  // ids before the first 16-byte boundary
+    const int quads = (n - head) / 4, tail = n - head - 4 * quads;
+    if (tid < head) mark(table[tid]);
+    if (tid < tail) mark(table[head + 4 * quads + tid]);
+    const uint4v* body = (const uint4v*)(table + head);
     constexpr int U = 8;
-    for (long long i0 = tid; i0 < n; i0 += (long long)U * kListThreads) {
-        int id[U];
+    for (int i0 = tid; i0 < quads; i0 += U * kListThreads) {
+        uint4v id[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) id[u] = i0 + (long long)u * kListThreads < n ? table[i0 + (long long)u * kListThreads] : -1;
+        for (int u = 0; u < U; ++u) {
+            id[u] = uint4v{~0u, ~0u, ~0u, ~0u};
+            if (quads - i0 > u * kListThreads) id[u] = body[i0 + u * kListThreads];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if ((unsigned)id[u] < (unsigned)n_pages) atomicOr(&bits[id[u] >> 5], 1u << (id[u] & 31));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) mark((int)id[u][x]);
     }
     __syncthreads();
 }
@@ -135,14 +148,31 @@ __device__ __forceinline__ void count_kept(const uint64_t* groups, int first, in
     }
 }
 
-// Their ids, ascending, from list[at] on.
+// Their ids, ascending, from list[at] on.  64 groups at a time, a lane has the bits of one.  Where all have few, every lane writes its own, bit by bit; else
+// the wavefront takes the groups in turn, a lane for a bit.
 template <typename F>
 __device__ __forceinline__ void list_kept(const uint64_t* groups, int first, int last, const F& keep, int* list, int at) {
+    constexpr int kFew = 16;
     const int lane = threadIdx.x & 63;
-    for (int g = first; g < last; ++g) {
-        const uint64_t b = keep(g, groups[g]);
-        if ((b >> lane) & 1) list[at + __popcll(b & ((1ull << lane) - 1))] = 64 * g + lane;
-        at += __popcll(b);
+    for (int g0 = first; g0 < last; g0 += 64) {
+        uint64_t mine = g0 + lane < last ? keep(g0 + lane, groups[g0 + lane]) : 0;
+        const int count = __popcll(mine), upto = wave_prefix(count);
+        if (!__any(count > kFew)) {
+            for (int to = at + upto - count; __any(mine != 0); ++to) {
+                if (mine) list[to] = 64 * (g0 + lane) + __builtin_ctzll(mine);
+                mine &= mine - 1;
+            }
+        } else {
+            int to = at;
+            const int end = min(last - g0, 64);
+            for (int i = 0; i < end; ++i) {
+                const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, i), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(mine >> 32), i);
+                const uint64_t bits = ((uint64_t)hi << 32) | lo;
+                if ((bits >> lane) & 1) list[to + (int)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0))] = 64 * (g0 + i) + lane;
+                to += __popcll(bits);
+            }
+        }
+        at += __builtin_amdgcn_readlane(upto, 63);
     }
 }
 
@@ -164,7 +194,7 @@ __global__ __launch_bounds__(kListThreads) void cache8_free_kernel(int* page_tab
         if ((tid & 63) == 0) lens[s] = 0;
     }
     __syncthreads();  // the rows are read below
-    mark_held((uint32_t*)bitmap, n_pages, page_table, (long long)n_seqs * max_pages);
+    mark_held((uint32_t*)bitmap, n_pages, page_table, n_seqs * max_pages);
     const int groups = (n_pages + 63) / 64, share = (groups + kListWaves - 1) / kListWaves;
     const int first = min(w * share, groups), last = min(first + share, groups);
     auto keep = [&](int g, uint64_t held) { return ~held & below(g, n_pages); };
@@ -176,7 +206,7 @@ __global__ __launch_bounds__(kListThreads) void cache8_free_kernel(int* page_tab
 }
 
 // Workspace of a compaction, ints: [0] the number of moves, then src, dst and the new id of a page that moves, n_pages each.
-__global__ __launch_bounds__(kListThreads) void cache8_compact_plan_kernel(const int* page_table, long long entries, int n_pages, int* n_used, int* ws) {
+__global__ __launch_bounds__(kListThreads) void cache8_compact_plan_kernel(const int* page_table, int entries, int n_pages, int* n_used, int* ws) {
     extern __shared__ __align__(16) uint64_t bitmap[];
     __shared__ int sums[kListWaves];
     const int tid = threadIdx.x, w = tid >> 6;
@@ -201,7 +231,7 @@ __global__ __launch_bounds__(kListThreads) void cache8_compact_plan_kernel(const
 }
 
 // Moves the pages and renames them in the table; workgroups share both, whose extent only the device knows.
-__global__ __launch_bounds__(kThreads) void cache8_compact_move_kernel(const PageArgs a, const int* page_table, int* new_table, long long entries,
+__global__ __launch_bounds__(kThreads) void cache8_compact_move_kernel(const PageArgs a, const int* page_table, int* new_table, int entries,
                                                                        const int* n_used, const int* ws) {
     const int moves = ws[0], used = *n_used, pieces = 2 * a.pieces + 1;
     const int *src = ws + 1, *dst = src + a.n_pages, *now = dst + a.n_pages;
@@ -257,7 +287,7 @@ hipError_t launch_cache8_compact(const flat_cache8& c, const int* page_table, in
                                  int* workspace, hipStream_t stream) {
     hipError_t e = allow_dynamic_lds((const void*)cache8_compact_plan_kernel, kMaxBitmap, &g_plan_lds);
     if (e != hipSuccess) return e;
-    const long long entries = (long long)n_seqs * max_pages;
+    const int entries = n_seqs * max_pages;  // fits: the C ABI checks
     hipLaunchKernelGGL(cache8_compact_plan_kernel, dim3(1), dim3(kListThreads), bitmap_bytes(c.n_pages), stream, page_table, entries, c.n_pages, n_used, workspace);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

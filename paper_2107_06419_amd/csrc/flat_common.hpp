@@ -88,6 +88,17 @@ __device__ __forceinline__ float wave_max(float x) {
     return __builtin_fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x121, 0xf, 0xf, true)));
 }
 
+// Inclusive sums over the lanes of a wavefront: within rows of 16 lanes, then the rows' totals carried on.
+__device__ __forceinline__ int wave_prefix(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // from the lane 1, 2, 4, 8 before, in the row
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // lane 15 of a row to the next one (rows 1 and 3)
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // lane 31 to the upper half
+    return x;
+}
+
 // Quotients n / d of 0 <= n < 2^31 by a divisor known when the kernel is launched: mul = ceil(2^(32+shift) / d) with 2^shift < d <=
 // 2^(shift+1), so mul < 2^32, mul d - 2^(32+shift) < d <= 2^(shift+1), and the error n (mul d - 2^(32+shift)) / (d 2^(32+shift)) stays below 1 / d.
 // A division by a kernel argument takes about 40 dependent scalar instructions (200 cycles at the start of every workgroup), this five.
