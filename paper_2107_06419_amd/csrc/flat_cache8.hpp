@@ -53,17 +53,17 @@ hipError_t launch_cache8_compact(const flat_cache8& c, const int* page_table, in
 // Attention over the cache (flat_cache8_fwd.hip).  A row block is rows_per_block of the Nq * (H / heads) rows that share a head of the cache;
 // an entry is a row block of a batch entry, and its keys are divided over one or more units, a workgroup per unit and head.
 struct Cache8Plan {
-    int rows_per_block;  // 32: the wavefronts of a workgroup share the keys of a block's rows; 128: each of four has 32 rows of its own
+    int rows_per_block;  // 16, 32: the wavefronts of a workgroup share the keys of a block's rows; 128: each of four has 32 rows of its own
     int row_blocks;      // per batch entry, for Nq queries
     int entries;         // B * row_blocks
     int tile_keys;       // what a kernel takes of the keys at a time: a power of two
-    int aim, limit;      // blocks of 32 rows: units aimed at over all entries, and the most there are (per head of the cache); 0: every entry is one unit
+    int aim, limit;      // blocks of 16 and 32 rows: units aimed at over all entries, and the most there are (per head of the cache); 0: every entry is one unit
     int least_tiles;     // that a unit has, unless its entry has fewer
     size_t parts_at;     // bytes of the workspace before the units' partial results
     size_t workspace_bytes;
 };
-// Keys of a step of one wavefront, blocks of 32 rows: 8 KiB of codes (16 at d = 256).
-constexpr int cache8_step_keys(int d) { return d == 32 ? 128 : d == 64 ? 64 : 32; }
+// Keys of a step of one wavefront, blocks of 16 and 32 rows.
+constexpr int cache8_step_keys(int rows, int d) { return rows == 16 || d == 64 ? 64 : d == 32 ? 128 : 32; }
 void cache8_plan(int B, int H, int heads, int Nq, int max_tokens, int d, Cache8Plan* out);  // host arithmetic only
 struct Cache8Attend {
     const void* Q;

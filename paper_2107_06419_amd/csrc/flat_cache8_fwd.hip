@@ -17,9 +17,9 @@ __device__ __forceinline__ bf16* row_of_o(const Cache8Args& a, const CacheEntry&
     const int pos = a.by_group.quotient(row), g = row - pos * a.group;
     return a.O + ((size_t)(t.b * (size_t)a.H + kvh * a.group + g) * a.Nq + pos) * D;
 }
-template <int D>
+template <int D, int ROWS>
 __device__ __forceinline__ float* part_of(const Cache8Args& a, int u, int kvh) {
-    return a.parts + (size_t)(u * (size_t)a.heads + kvh) * (32 * (D + 2));
+    return a.parts + (size_t)(u * (size_t)a.heads + kvh) * (ROWS * (D + 2));
 }
 __device__ __forceinline__ floatx2 four_bf16(const floatx4& y, float by) {
     floatx2 out;
@@ -28,21 +28,28 @@ __device__ __forceinline__ floatx2 four_bf16(const floatx4& y, float by) {
     return out;
 }
 
-// ---- Few rows: up to 32 of the Nq * group rows that share a head of the cache.  The four wavefronts of a workgroup take the unit's steps of
-// 32 TPS keys in turn, with K and V widened from their codes in registers: no LDS and no barrier before the end.  What bounds it is the reading of the
-// codes: a wavefront asks for the next step's as soon as this one's are widened, 8 KiB a step at d = 32 to 128, so that 64 KiB a compute unit are on their way.
+// ---- Few rows: up to ROWS = 16 or 32 of the Nq * group rows that share a head of the cache.  The four wavefronts of a workgroup take the unit's steps
+// of TPS tiles in turn, with K and V widened from their codes in registers: no LDS and no barrier before the end.  What bounds it is the reading of the
+// codes, and where few workgroups run the instructions of a wavefront: a wavefront asks for the next codes as soon as it has widened these.
+//
+// A tile is 64 / ROWS blocks: 32 keys on the 32 x 32 x 16 MFMA, 64 keys on the 16 x 16 x 32 one, four products of 16 keys each.  With 16 rows the tokens of
+// K's operand are dealt out likewise, row m of product t is block m / 4, token 4 t + m % 4, and a lane again ends up with the 16 tokens of one block.  The lanes'
+// work per key is half that of 32 rows: 16 workgroups over 4096 keys, 32 rows -> 16, d = 64 18.9 -> 14.8 us, d = 128 26.8 -> 20.1.
 constexpr int NW = 4;  // wavefronts of a workgroup, in both kernels
 
 // DIVIDED: the entries' keys are divided over units; else a unit is an entry, and its page ids are fetched along with its lengths.
-template <int D, int FMT, bool DIVIDED>
+template <int D, int ROWS, int FMT, bool DIVIDED>
 __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_kernel(const Cache8Args a, int lds_rows) {
-    constexpr int J = D / 32;             // 16-byte pieces of a K row per wave half, and 32-channel groups of V
-    constexpr int TPS = cache8_step_keys(D) / 32, BPS = 2 * TPS, GROUP = 64 / BPS;  // tiles and blocks of a step; steps whose blocks 64 lanes know
-    constexpr int AHEAD = D == 256 ? 1 : 2;  // steps whose codes are on their way
-    constexpr int RS = D + 4;             // row stride of the merge buffer, floats: spreads the rows over the banks
+    constexpr int LG = 64 / ROWS;                                 // lane groups: each has one block of a tile
+    constexpr int NQ = D / (16 * LG);                             // contraction pieces of a row, 16 channels per lane group
+    constexpr int KL = ROWS == 32 ? NQ : 4 * NQ, VL = D / ROWS;   // 16-byte loads of K and V per lane and tile
+    constexpr int TPS = cache8_step_keys(ROWS, D) / (16 * LG), BPS = LG * TPS, GROUP = 64 / BPS;  // tiles and blocks of a step; steps whose blocks 64 lanes know
+    constexpr int RS = D + 4;                                     // row stride of the merge buffer, floats: spreads the rows over the banks
+    typedef std::conditional_t<ROWS == 32, floatx16, floatx4> acc_t;
+    constexpr int AR = ROWS == 32 ? 16 : 4;                       // its registers
     extern __shared__ __align__(16) float lds[];  // [NW][lds_rows][RS], then statistics
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int half = lane >> 5, col = lane & 31;
+    const int grp = lane / ROWS, col = lane % ROWS;
     const int id = blockIdx.x, u = a.by_heads.quotient(id), kvh = id - u * a.heads;
 
     CacheUnit unit;
@@ -78,13 +85,13 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
     // the rows: row = position * group + query head of the group
     const int row = t.row0 + col, pos = a.by_group.quotient(row);
     const bool has_row = row < t.rows;
-    bf16x8 q[2 * J];
+    bf16x8 q[2 * NQ];
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
+    for (int j = 0; j < NQ; ++j) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             q[2 * j + i] = bf16x8{};
-            if (has_row) q[2 * j + i] = *(const bf16x8*)(row_of_o<D>(a, t, kvh, row) - a.O + a.Q + 32 * j + 16 * half + 8 * i);
+            if (has_row) q[2 * j + i] = *(const bf16x8*)(row_of_o<D>(a, t, kvh, row) - a.O + a.Q + 16 * (LG * j + grp) + 8 * i);
         }
     }
     const int seen = !has_row ? t.len : a.causal ? min(max(pos + 1 + t.len - t.q_len, 0), t.len) : t.len;  // keys that this row sees
@@ -94,35 +101,42 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
     int next_page = -1;
     int now_at = max(now.e, 0);  // of the group that the next loads are for; holes read block 0, and what they read counts for nothing
     uint64_t lacking = __ballot(now.there < 16);  // blocks of the group of which a token or more is not there
-    const uint8_t *k_lane = a.k + (4 * (col >> 3) + (col & 3)) * 16 + half * 256, *v_lane = a.v + col * 16;
-    uint4v kc[AHEAD][TPS][J], vc[AHEAD][TPS][J];
-    auto load = [&](const uint8_t* mine, int e, int at, int second, uint4v (&x)[TPS][J]) __attribute__((always_inline)) {
+    // the lane's place in a block, and which block of the tile: K as the A operand's rows, V by lane group
+    const int k_block = ROWS == 32 ? (col >> 2) & 1 : col >> 2;
+    const uint8_t *k_lane = a.k + (ROWS == 32 ? 4 * (col >> 3) + (col & 3) : col & 3) * 16 + grp * 256, *v_lane = a.v + col * 16;
+    uint4v kc[TPS][KL], vc[TPS][VL];
+    auto block_at = [&](int i, int t2, int block) __attribute__((always_inline)) {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * (BPS * (i % GROUP) + LG * t2 + block), now_at) * (16 * D);
+    };
+    auto load_k = [&](int i) __attribute__((always_inline)) {
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
-            const uint8_t* p = mine + (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * (BPS * at + 2 * t2 + second), e) * (16 * D);
+            const uint8_t* p = k_lane + block_at(i, t2, k_block);
 #pragma unroll
-            for (int j = 0; j < J; ++j) x[t2][j] = *(const uint4v*)(p + 512 * j);
+            for (int x = 0; x < KL; ++x) kc[t2][x] = *(const uint4v*)(p + (ROWS == 32 ? 512 * x : 1024 * (x / 4) + 64 * (x % 4)));
         }
     };
-    auto load_k = [&](int i, int set) __attribute__((always_inline)) { load(k_lane, now_at, i % GROUP, (col >> 2) & 1, kc[set]); };
-    auto load_v = [&](int i, int set) __attribute__((always_inline)) { load(v_lane, now_at, i % GROUP, half, vc[set]); };
+    auto load_v = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int t2 = 0; t2 < TPS; ++t2) {
+            const uint8_t* p = v_lane + block_at(i, t2, grp);
+#pragma unroll
+            for (int x = 0; x < VL; ++x) vc[t2][x] = *(const uint4v*)(p + 16 * ROWS * x);
+        }
+    };
 
-    floatx16 o[J];
+    acc_t o[VL];
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int j = 0; j < VL; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
+        for (int r = 0; r < AR; ++r) o[j][r] = 0.f;
     RowState st{-INFINITY, 0.f, 0.f};
 
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-        if (i < n_mine) {
-            load_k(i, i);
-            load_v(i, i);
-        }
+    if (n_mine > 0) {
+        load_k(0);
+        load_v(0);
     }
-    auto step = [&](int i, auto which) __attribute__((always_inline)) {
-        constexpr int SET = decltype(which)::value;
+    auto step = [&](int i) __attribute__((always_inline)) {  // (as the loop's own body it came out a tenth slower, by the order the compiler gives it)
         const int at = i % GROUP;
         // pages and scales of the next GROUP steps: fetched over these, so that their two round trips are not waited for
         if (at == 0 && i + GROUP < n_mine) next_page = page_of(i / GROUP + 1);
@@ -130,18 +144,18 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
         float c[TPS], vs_log2[TPS], vs_inv[TPS];
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
-            const int from = 4 * (BPS * at + 2 * t2 + half);
+            const int from = 4 * (BPS * at + LG * t2 + grp);
             c[t2] = value_of_lane(from, now.ks);
             vs_log2[t2] = value_of_lane(from, now.vs_log2);
             vs_inv[t2] = value_of_lane(from, now.vs_inv);
         }
-        const int key0 = (first + NW * i) * (32 * TPS);
-        const bool edge = key0 + 32 * TPS > all_see || ((lacking >> (BPS * at)) & ((1ull << BPS) - 1)) != 0;
+        const int key0 = (first + NW * i) * (16 * BPS);
+        const bool edge = key0 + 16 * BPS > all_see || ((lacking >> (BPS * at)) & ((1ull << BPS) - 1)) != 0;
         int there[TPS], hole[TPS];
         if (edge) {
 #pragma unroll
             for (int t2 = 0; t2 < TPS; ++t2) {
-                const int from = 4 * (BPS * at + 2 * t2 + half);
+                const int from = 4 * (BPS * at + LG * t2 + grp);
                 there[t2] = __builtin_amdgcn_ds_bpermute(from, now.there);
                 hole[t2] = __builtin_amdgcn_ds_bpermute(from, now.e);
             }
@@ -150,32 +164,46 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
             now = next;
             lacking = __ballot(now.there < 16);
         }
-        if (at == GROUP - AHEAD) now_at = max(next.e, 0);
+        now_at = at == GROUP - 1 ? max(next.e, 0) : now_at;
 
-        floatx16 s[TPS];
+        float s[TPS][16];  // logits of the lane's row and block, token by token
         int visible[TPS];
         float top = -INFINITY;
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[t2][r] = 0.f;
+            for (int y = 0; y < KL / NQ; ++y) {
+                acc_t z;
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[SET][t2][j][0], kc[SET][t2][j][1]), q[2 * j], s[t2]);
-                s[t2] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(kc[SET][t2][j][2], kc[SET][t2][j][3]), q[2 * j + 1], s[t2]);
-                if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);  // the widening takes registers: not all of it at once
+                for (int r = 0; r < AR; ++r) z[r] = 0.f;
+#pragma unroll
+                for (int j = 0; j < NQ; ++j) {
+                    const uint4v k = kc[t2][KL / NQ * j + y];
+                    if constexpr (ROWS == 32) {
+                        z = mfma_bf16_32x32x16(codes_to_bf16<FMT>(k[0], k[1]), q[2 * j], z);
+                        z = mfma_bf16_32x32x16(codes_to_bf16<FMT>(k[2], k[3]), q[2 * j + 1], z);
+                    } else {
+                        z = mfma_bf16_16x16x32(codes_to_bf16<FMT>(k[0], k[1]), q[2 * j], z);
+                        z = mfma_bf16_16x16x32(codes_to_bf16<FMT>(k[2], k[3]), q[2 * j + 1], z);
+                    }
+                    if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);  // the widening takes registers: not all of it at once
+                }
+#pragma unroll
+                for (int r = 0; r < AR; ++r) s[t2][AR * y + r] = z[r];
             }
         }
-        // K's registers are free: the codes of the step after next into them, and V's below
-        if (i + AHEAD < n_mine) load_k(i + AHEAD, SET);
+        // K's registers are free: the next step's codes into them, and V's below.  Never skipped (behind the last step, the last one's once more): if they
+        // could be, the compiler would not count on them being on their way, and wait for more than it needs.  (Two steps ahead instead of one: no faster at
+        // 16 workgroups, slower at 1024 by what short walks fetch in vain, 128 keys, d = 64, 5.7 -> 7.5 us.)
+        load_k(min(i + 1, n_mine - 1));
 #pragma unroll
         for (int t2 = 0; t2 < TPS; ++t2) {
             visible[t2] = 16;
             float most;
             if (edge) {
-                visible[t2] = hole[t2] < 0 ? 0 : min(max(seen - key0 - 32 * t2 - kCacheBlock * half, 0), 16);
+                visible[t2] = hole[t2] < 0 ? 0 : min(max(seen - key0 - kCacheBlock * (LG * t2 + grp), 0), 16);
 #pragma unroll
-                for (int j = 0; j < J; ++j) vc[SET][t2][j] = clear_behind(vc[SET][t2][j], there[t2]);
+                for (int j = 0; j < VL; ++j) vc[t2][j] = clear_behind(vc[t2][j], there[t2]);
                 most = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) most = __builtin_fmaxf(most, r < visible[t2] ? s[t2][r] : -INFINITY);
@@ -188,15 +216,15 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
             }
             top = __builtin_fmaxf(top, most);
         }
-        top = halves_max(top);
+        top = row_max<ROWS>(top);
         if (__any(top > st.m + kRescaleAbove)) {
             const float up = __builtin_fmaxf(st.m, top), sub = up == -INFINITY ? 0.f : up;
             const float by = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.sub - sub);
             st.l *= by;
 #pragma unroll
-            for (int j = 0; j < J; ++j)
+            for (int j = 0; j < VL; ++j)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) o[j][r] *= by;
+                for (int r = 0; r < AR; ++r) o[j][r] *= by;
             st.m = up;
             st.sub = sub;
         }
@@ -206,36 +234,38 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
             if (edge) tile_probabilities<true>(s[t2], c[t2], vs_log2[t2], vs_inv[t2], st.sub, visible[t2], &lo, &hi, &st.l);
             else tile_probabilities<false>(s[t2], c[t2], vs_log2[t2], vs_inv[t2], st.sub, 16, &lo, &hi, &st.l);
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[SET][t2][j][0], vc[SET][t2][j][1]), lo, o[j]);
-                o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(vc[SET][t2][j][2], vc[SET][t2][j][3]), hi, o[j]);
+            for (int j = 0; j < VL; ++j) {
+                const uint4v v = vc[t2][j];
+                if constexpr (ROWS == 32) {
+                    o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(v[0], v[1]), lo, o[j]);
+                    o[j] = mfma_bf16_32x32x16(codes_to_bf16<FMT>(v[2], v[3]), hi, o[j]);
+                } else {
+                    o[j] = mfma_bf16_16x16x32(codes_to_bf16<FMT>(v[0], v[1]), lo, o[j]);
+                    o[j] = mfma_bf16_16x16x32(codes_to_bf16<FMT>(v[2], v[3]), hi, o[j]);
+                }
                 if (FMT == FLAT_CACHE8_INT8) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (i + AHEAD < n_mine) load_v(i + AHEAD, SET);
+        load_v(min(i + 1, n_mine - 1));
     };
-    for (int i = 0; i < n_mine;) {
-        step(i, std::integral_constant<int, 0>());
-        if (AHEAD > 1 && ++i < n_mine) step(i, std::integral_constant<int, AHEAD - 1>());
-        ++i;
-    }
-    st.l = halves_sum(st.l);
+    for (int i = 0; i < n_mine; ++i) step(i);
+    st.l = row_sum<ROWS>(st.l);
 
     // the wavefronts' parts: every one scales its own to the common maximum, then all add up
-    float* stat = lds + NW * lds_rows * RS;  // [NW][2][32]
-    if (half == 0) {
-        stat[w * 64 + col] = st.m;
-        stat[w * 64 + 32 + col] = st.l;
+    float* stat = lds + NW * lds_rows * RS;  // [NW][2][ROWS]
+    if (grp == 0) {
+        stat[w * 2 * ROWS + col] = st.m;
+        stat[w * 2 * ROWS + ROWS + col] = st.l;
     }
     __syncthreads();
     auto joined = [&](int r, float* top, float* sum) __attribute__((always_inline)) {
         float m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) m = __builtin_fmaxf(m, stat[i * 64 + r]);
+        for (int i = 0; i < NW; ++i) m = __builtin_fmaxf(m, stat[i * 2 * ROWS + r]);
         float l = 0.f;
 #pragma unroll
         for (int i = 0; i < NW; ++i) {
-            const float mi = stat[i * 64 + r], li = stat[i * 64 + 32 + r];
+            const float mi = stat[i * 2 * ROWS + r], li = stat[i * 2 * ROWS + ROWS + r];
             l += mi == -INFINITY ? li : li * __builtin_amdgcn_exp2f(mi - m);  // without a maximum the sum is 0, or not a number
         }
         *top = m;
@@ -244,21 +274,21 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
     float top, sum;
     joined(col, &top, &sum);
     const float mine = st.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - top);
-    const int rows = min(t.rows - t.row0, 32);
+    const int rows = min(t.rows - t.row0, ROWS);
     if (col < rows) {
 #pragma unroll
-        for (int j = 0; j < J; ++j)
+        for (int j = 0; j < VL; ++j)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
+            for (int x = 0; x < AR / 4; ++x) {
                 floatx4 y;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) y[r] = o[j][4 * x + r] * mine;
-                *(floatx4*)(lds + (w * lds_rows + col) * RS + 32 * j + 8 * x + 4 * half) = y;
+                *(floatx4*)(lds + (w * lds_rows + col) * RS + ROWS * j + 8 * x + 4 * grp) = y;
             }
     }
     __syncthreads();
     constexpr int Q4 = D / 4;  // 16-byte groups of columns per row
-    float* part = part_of<D>(a, u, kvh);
+    float* part = part_of<D, ROWS>(a, u, kvh);
     for (int x = tid; x < rows * Q4; x += 64 * NW) {
         const int r = x / Q4, c4 = x - r * Q4;
         floatx4 y = *(const floatx4*)(lds + r * RS + 4 * c4);
@@ -273,8 +303,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
         *(floatx2*)(row_of_o<D>(a, t, kvh, t.row0 + r) + 4 * c4) = four_bf16(y, l == 0.f ? 0.f : 1.0f / l);
     }
     if (DIVIDED && unit.n > 1 && tid < rows) {
-        part[32 * D + tid] = top;
-        part[32 * D + 32 + tid] = sum;
+        part[ROWS * D + tid] = top;
+        part[ROWS * D + ROWS + tid] = sum;
     }
     if (DIVIDED && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
 }
@@ -520,9 +550,9 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(const Cache8Args a) {
     const int r = 4 * blockIdx.y + (threadIdx.x >> 6), row = t.row0 + r;
     if (row >= t.rows || unit.y == 1) return;
     const int n = unit.y, c4 = lane % Q4, first = lane / Q4 < LANES ? lane / Q4 : n;  // d = 96: some lanes have no column
-    const size_t size = 32 * (D + 2), stride = size * a.heads;
+    const size_t size = (size_t)a.rows_per_block * (D + 2), stride = size * a.heads;
     const float* base = a.parts + ((size_t)unit.x * a.heads + kvh) * size;
-    const float *m_of = base + 32 * D + r, *o_of = base + (size_t)r * D + 4 * c4;
+    const float *m_of = base + a.rows_per_block * D + r, *o_of = base + (size_t)r * D + 4 * c4;
     floatx4 ahead[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
@@ -537,7 +567,7 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(const Cache8Args a) {
     for (int s0 = 0; s0 < n; s0 += 64) {
         float wt = 0.f;
         if (s0 + lane < n) {
-            const float m = m_of[(s0 + lane) * stride], l = m_of[(s0 + lane) * stride + 32];
+            const float m = m_of[(s0 + lane) * stride], l = m_of[(s0 + lane) * stride + a.rows_per_block];
             wt = part_weight(m, l, top);
             L += wt * l;
         }
@@ -574,9 +604,9 @@ __global__ __launch_bounds__(256) void cache8_merge_many_kernel(const Cache8Args
     const int r = blockIdx.y, row = t.row0 + r;
     if (row >= t.rows || unit.y == 1) return;
     const int n = unit.y;
-    const size_t size = 32 * (D + 2), stride = size * a.heads;
+    const size_t size = (size_t)a.rows_per_block * (D + 2), stride = size * a.heads;
     const float* base = a.parts + ((size_t)unit.x * a.heads + kvh) * size;
-    const float* m_of = base + 32 * D + r;
+    const float* m_of = base + a.rows_per_block * D + r;
     const int c4 = tid % Q4, first = tid / Q4;
     const float* o_of = base + (size_t)r * D + COLS * blockIdx.z + 4 * c4;
 
@@ -589,7 +619,7 @@ __global__ __launch_bounds__(256) void cache8_merge_many_kernel(const Cache8Args
     float top = -INFINITY, m0 = -INFINITY, l0 = 0.f;
     if (tid < n) {
         m0 = m_of[tid * stride];
-        l0 = m_of[tid * stride + 32];
+        l0 = m_of[tid * stride + a.rows_per_block];
     }
     top = m0;
     for (int s = tid + THREADS; s < n; s += THREADS) top = __builtin_fmaxf(top, m_of[s * stride]);
@@ -604,7 +634,7 @@ __global__ __launch_bounds__(256) void cache8_merge_many_kernel(const Cache8Args
         if (s0 + tid < n) {
             if (s0) {
                 m0 = m_of[(s0 + tid) * stride];
-                l0 = m_of[(s0 + tid) * stride + 32];
+                l0 = m_of[(s0 + tid) * stride + a.rows_per_block];
             }
             const float wt = part_weight(m0, l0, top);
             wts[tid] = wt;
@@ -634,17 +664,21 @@ __global__ __launch_bounds__(256) void cache8_merge_many_kernel(const Cache8Args
     *(floatx2*)(row_of_o<D>(a, t, kvh, row) + COLS * blockIdx.z + 4 * c4) = four_bf16(acc, L == 0.f ? 0.f : 1.0f / L);
 }
 
-template <int D, int FMT, bool DIVIDED>
+template <int D, int ROWS, int FMT, bool DIVIDED>
 hipError_t launch_few(const Cache8Args& args, hipStream_t stream) {
     static std::atomic<uint64_t> lds_allowed{0};
-    constexpr auto lds_bytes = [](int rows) { return (NW * rows * (D + 4) + NW * 64) * (int)sizeof(float); };
-    static_assert(lds_bytes(32) <= 160 * 1024, "the wavefronts' results must fit the LDS");
-    const hipError_t e = allow_dynamic_lds((const void*)cache8_few_rows_kernel<D, FMT, DIVIDED>, lds_bytes(32), &lds_allowed);
+    constexpr auto lds_bytes = [](int rows) { return (NW * rows * (D + 4) + NW * 2 * ROWS) * (int)sizeof(float); };
+    static_assert(lds_bytes(ROWS) <= 160 * 1024, "the wavefronts' results must fit the LDS");
+    const hipError_t e = allow_dynamic_lds((const void*)cache8_few_rows_kernel<D, ROWS, FMT, DIVIDED>, lds_bytes(ROWS), &lds_allowed);
     if (e != hipSuccess) return e;
-    const int rows = args.Nq * args.group < 32 ? args.Nq * args.group : 32;
+    const int rows = args.Nq * args.group < ROWS ? args.Nq * args.group : ROWS;
     const unsigned units = (unsigned)(DIVIDED ? args.limit : args.entries);
-    hipLaunchKernelGGL((cache8_few_rows_kernel<D, FMT, DIVIDED>), dim3(units * (unsigned)args.heads), dim3(64 * NW), lds_bytes(rows), stream, args, rows);
+    hipLaunchKernelGGL((cache8_few_rows_kernel<D, ROWS, FMT, DIVIDED>), dim3(units * (unsigned)args.heads), dim3(64 * NW), lds_bytes(rows), stream, args, rows);
     return hipGetLastError();
+}
+template <int D, int ROWS, int FMT>
+hipError_t launch_few(const Cache8Args& args, hipStream_t stream) {
+    return args.limit ? launch_few<D, ROWS, FMT, true>(args, stream) : launch_few<D, ROWS, FMT, false>(args, stream);
 }
 
 template <int D, int FMT>
@@ -660,7 +694,7 @@ hipError_t launch_rows(const Cache8Args& args, hipStream_t stream) {
 
 template <int D>
 hipError_t launch_merge(const Cache8Args& args, hipStream_t stream) {
-    const int rows = args.Nq * args.group < 32 ? args.Nq * args.group : 32;  // that a block has at most
+    const int rows = args.Nq * args.group < args.rows_per_block ? args.Nq * args.group : args.rows_per_block;  // that a block has at most
     const unsigned grid = (unsigned)args.entries * (unsigned)args.heads;
     if (args.limit <= 16 * args.entries) hipLaunchKernelGGL((cache8_merge_kernel<D>), dim3(grid, (unsigned)(rows + 3) / 4), dim3(256), 0, stream, args);
     else hipLaunchKernelGGL((cache8_merge_many_kernel<D>), dim3(grid, (unsigned)rows, D / 32), dim3(256), 0, stream, args);
@@ -669,10 +703,10 @@ hipError_t launch_merge(const Cache8Args& args, hipStream_t stream) {
 
 template <int D, int FMT>
 hipError_t launch(const Cache8Args& args, hipStream_t stream) {
-    hipError_t e;
-    if (args.rows_per_block > 32) e = launch_rows<D, FMT>(args, stream);
-    else if (args.limit) e = launch_few<D, FMT, true>(args, stream);
-    else e = launch_few<D, FMT, false>(args, stream);
+    hipError_t e = hipErrorInvalidValue;
+    if (args.rows_per_block == 128) e = launch_rows<D, FMT>(args, stream);
+    else if (args.rows_per_block == 32) e = launch_few<D, 32, FMT>(args, stream);
+    else if constexpr (D % 64 == 0) e = launch_few<D, 16, FMT>(args, stream);
     return e != hipSuccess || args.limit == 0 ? e : launch_merge<D>(args, stream);
 }
 

@@ -140,17 +140,17 @@ __device__ __forceinline__ CacheBlock cache_block(const Cache8Args& a, int kvh, 
 // x of lane (byte address / 4).
 __device__ __forceinline__ float value_of_lane(int at, float x) { return __builtin_bit_cast(float, __builtin_amdgcn_ds_bpermute(at, __builtin_bit_cast(int, x))); }
 
-// The running state of a row's softmax, in both halves of the wavefront: reference maximum (log2 units), what is subtracted (0 until there is one), and the
-// sum of this half's keys.
+// The running state of a row's softmax, in every lane that has it: reference maximum (log2 units), what is subtracted (0 until there is one), and the
+// sum of this lane's keys.
 struct RowState {
     float m, sub, l;
 };
 constexpr int kRescaleAbove = 8;  // log2: the reference maximum rises only when a logit is this far above it, so p stays below 2^8 and exact to rounding
 
-// Probabilities of a 32-key tile: s holds the logits of the lane's row and block.  c: the block's key scale; the result is p * vs in
+// Probabilities of a tile: s holds the logits of the lane's row and block, token by token.  c: the block's key scale; the result is p * vs in
 // bf16, and *sum gets the sum of the block's p.  visible: tokens of the block that the row sees (all if !EDGE).
-template <bool EDGE>
-__device__ __forceinline__ void tile_probabilities(const floatx16& s, float c, float vs_log2, float vs_inv, float sub, int visible, bf16x8* lo, bf16x8* hi, float* l) {
+template <bool EDGE, typename S>
+__device__ __forceinline__ void tile_probabilities(const S& s, float c, float vs_log2, float vs_inv, float sub, int visible, bf16x8* lo, bf16x8* hi, float* l) {
     constexpr uint32_t kOnes = 0x3f803f80u;
     const float b = vs_log2 - sub;
     uint4v plo, phi;
@@ -170,6 +170,32 @@ __device__ __forceinline__ void tile_probabilities(const floatx16& s, float c, f
     *lo = __builtin_bit_cast(bf16x8, plo);
     *hi = __builtin_bit_cast(bf16x8, phi);
     if (!EDGE || visible > 0) *l = __builtin_fmaf(sum, vs_inv, *l);  // a scale that is no number is none of a row that does not see the block
+}
+
+// v_mfma_f32_16x16x32_bf16:  D[16x16] += A[16x32] * B[32x16].  A: lane l holds row (l % 16), contraction indices 8 (l / 16) .. + 7; B: column (l % 16), the
+// same indices; C/D: column (l % 16), register r is row 4 (l / 16) + r.
+__device__ __forceinline__ floatx4 mfma_bf16_16x16x32(bf16x8 a, bf16x8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// Largest value, and sum, over the lanes that have a row: l and l ^ 32, and where a tile has 16 rows l ^ 16 too.
+template <int ROWS>
+__device__ __forceinline__ float row_max(float x) {
+    x = halves_max(x);
+    if constexpr (ROWS == 16) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, x);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = __builtin_fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+    }
+    return x;
+}
+template <int ROWS>
+__device__ __forceinline__ float row_sum(float x) {
+    x = halves_sum(x);
+    if constexpr (ROWS == 16) {
+        const uint32_t u = __builtin_bit_cast(uint32_t, x);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+    }
+    return x;
 }
 
 // Eight codes as bf16, exactly: e4m3 has 4 significant bits, int8 8.

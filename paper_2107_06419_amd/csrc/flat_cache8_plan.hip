@@ -8,35 +8,36 @@ namespace flat {
 // Which kernel an attention call takes, and whether the keys of its entries are divided over workgroups.  Figures: e4m3, 4 query heads to a head of the cache,
 // us, a hipGraph of ten calls; BH = batch entries * heads of the cache.
 //
-// Blocks of 32 rows, whose keys the four wavefronts of a workgroup share, or of 128 rows, whose tiles are widened once for four wavefronts: the latter
+// Blocks of 16 or 32 rows, whose keys the four wavefronts of a workgroup share, or of 128 rows, whose tiles are widened once for four wavefronts: the latter
 // need 512 workgroups (256 at d = 256, where one fills a compute unit) to be ahead, whatever the number of keys.  BH = 32, 2048 rows, d = 128 (512 blocks): 512 keys 37.3 against 36.6,
 // 2048 97 / 94, 8192 323 / 300; BH = 128, 512 rows, 8192 keys 353 / 317; half as many, BH = 8, 2048 rows, 8192 keys 93 / 113; d = 256, 256 blocks of 2048 keys 128 / 117, 128 blocks 61 / 86.
 //
 // Dividing costs a launch and the parts' way through memory, 5 us and more, and gives shorter walks over the keys and even shares of a ragged batch.  A workgroup takes
-// about 5.5 us and kRound per round of its four wavefronts, but no less than the memory takes for the codes of all of them at 5.2 TB/s (counted at 0.6: a batch is as often
-// ragged as not).  What dividing saves is the difference, round by round.  One row group, undivided / divided: d = 128, BH = 16, 1024 keys 10.9 / 11.0, 4096 27.3 / 12.7; BH = 128, 2048
-// keys 17.8 / 21.5, 4096 30.3 / 31.7, ragged up to 4096 28.3 / 23.8; BH = 256, 4096 keys 50.2 / 56.9, ragged 38.6 / 38.0; d = 64, BH = 64, 2048 keys 12.9 / 12.6, 8192 35 / 22.
+// about 5.5 us and `round` per step of its four wavefronts, but no less than the memory takes for the codes of all of them at 5.2 TB/s, counted at 0.45: a batch is as often
+// ragged as not, and its longest walk counts.  What dividing saves is the difference, step by step.  Up to 16 rows, ragged batches of 0.1 to 1 times the keys, undivided / divided: d = 64,
+// BH = 64, 2048 keys 10.7 / 10.8, 4096 17.3 / 13.8; BH = 128, 2048 11.3 / 13.5, 16384 59 / 36; BH = 256, 16384 70 / 67; d = 128, BH = 64, 2048 14.1 / 14.6, 4096 21.7 / 17.6; BH = 128, 4096 22.1 /
+// 22.0, 16384 90 / 65; BH = 256, 4096 33.6 / 35.6; d = 256, BH = 64, 1024 16.9 / 15.7; BH = 128, 1024 17.7 / 18.7, 4096 51 / 40.
 void cache8_plan(int B, int H, int heads, int Nq, int max_tokens, int d, Cache8Plan* out) {
     constexpr int kLeastKeys = 256;
     const int held = d == 256 ? 256 : 512;  // workgroups that 256 compute units hold at once
     const long long rows = (long long)Nq * (H / heads);
-    out->rows_per_block = rows > 32 && (rows + 127) / 128 * B * heads >= held ? 128 : 32;
+    out->rows_per_block = rows > 32 && (rows + 127) / 128 * B * heads >= held ? 128 : rows <= 16 && d % 64 == 0 ? 16 : 32;
     out->row_blocks = (int)((rows + out->rows_per_block - 1) / out->rows_per_block);
     const long long entries = (long long)B * out->row_blocks, grid = entries * heads;
     out->entries = (int)entries;
-    out->tile_keys = out->rows_per_block > 32 ? 64 : cache8_step_keys(d);
+    out->tile_keys = out->rows_per_block > 32 ? 64 : cache8_step_keys(out->rows_per_block, d);
     out->least_tiles = kLeastKeys / out->tile_keys;
     out->aim = out->limit = 0;
     out->parts_at = out->workspace_bytes = 0;
     if (out->rows_per_block > 32 || grid >= held) return;
-    const double kRound = d == 32 ? 1.5 : d == 64 ? 0.95 : d == 96 ? 0.64 : d == 128 ? 0.7 : 1.22;           // us
+    const double round = out->rows_per_block == 16 ? (d == 64 ? 0.62 : d == 128 ? 0.95 : 2.4) : d == 32 ? 1.5 : d == 64 ? 0.87 : d == 96 ? 0.64 : d == 128 ? 0.67 : 1.2;  // us
     const long long round_keys = 4 * out->tile_keys, rounds = (max_tokens + round_keys - 1) / round_keys;
-    const double memory = 0.6 * (double)grid * (double)(round_keys * 2 * d) / 5.2e6;
-    if ((double)rounds * (kRound - memory) <= 5.5 + (double)(rows < 32 ? rows : 32) / 16.0) return;
+    const double memory = 0.45 * (double)grid * (double)(round_keys * 2 * d) / 5.2e6;
+    if ((double)rounds * (round - memory) <= 5.5 + (double)(rows < 32 ? rows : 32) / 16.0) return;
     out->aim = held / heads > entries ? held / heads : (int)entries;
     out->limit = 2 * entries <= out->aim ? out->aim : out->aim + (int)entries;
     out->parts_at = ((size_t)entries * 8 + 15) / 16 * 16;
-    out->workspace_bytes = out->parts_at + (size_t)out->limit * heads * 32 * (d + 2) * sizeof(float);
+    out->workspace_bytes = out->parts_at + (size_t)out->limit * heads * out->rows_per_block * (d + 2) * sizeof(float);
 }
 
 }  // namespace flat
