@@ -318,6 +318,9 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     constexpr int MINE = (PAIRS + NW - 1) / NW;         // of a wavefront: pairs w, w + NW, ...
     constexpr int BUF = PAIRS * 2 * 1024;               // bytes of a tile
     constexpr int GROUP = 16;                           // tiles whose blocks 64 lanes know
+    // The next tile's widening beside Q K^T, or beside P V: 2 x 2048 queries over 16384 keys, d = 64, 345 us against 362, d = 256 (1024 over 8192) 314 / 325, 8 x 512
+    // over 4096, d = 96, 135 / 138; d = 128 566 / 552.  (Hints to the compiler how to mix MFMAs, vector work and LDS reads: 0 to 5 % slower at d = 128.)
+    constexpr bool kWidenFirst = D != 128;
     extern __shared__ __align__(16) uint8_t smem[];
     float* scales = (float*)(smem + 2 * BUF);           // [2][64 blocks][4]: ks, vs_log2, vs_inv, tokens there as int (-1: a hole)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -455,6 +458,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
         const uint64_t here = (lacking >> (4 * at)) & 15, after = at == GROUP - 1 ? lacking_next & 15 : (lacking >> (4 * at + 4)) & 15;
         return i + 2 < n && 64 * i + 64 <= all_see && (here | after) == 0;
     };
+    bool ahead = false;  // whether the next tile is widened and the one after it asked for
     for (int i = 0; i < n;) {
         look_ahead(i);
         while (plain(i)) {
@@ -463,6 +467,11 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
             const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + half);
             const floatx4 x0 = *(const floatx4*)sc, x1 = *(const floatx4*)(sc + 8);
             floatx16 s[2];
+            if (kWidenFirst) {
+                widen(i + 1, buf ^ 1, true);
+                load(i + 2);
+                ahead = true;
+            }
             logits(frag, s);
             float top[2];
 #pragma unroll
@@ -479,16 +488,22 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
             tile_probabilities<false>(s[0], x0[0], x0[1], x0[2], st.sub, 16, &p[0], &p[1], &st.l);
             attend(frag, 0, p);
             tile_probabilities<false>(s[1], x1[0], x1[1], x1[2], st.sub, 16, &p[0], &p[1], &st.l);
-            widen(i + 1, buf ^ 1, true);
-            load(i + 2);
+            if (!kWidenFirst) {
+                widen(i + 1, buf ^ 1, true);
+                load(i + 2);
+            }
             attend(frag, 1, p);
+            ahead = false;
             done(i);
             look_ahead(++i);
         }
         if (i >= n) break;
         const int buf = i & 1, key0 = 64 * i;
-        if (i + 1 < n) widen(i + 1, buf ^ 1, false);
-        if (i + 2 < n) load(i + 2);
+        if (!ahead) {
+            if (i + 1 < n) widen(i + 1, buf ^ 1, false);
+            if (i + 2 < n) load(i + 2);
+        }
+        ahead = false;
         if (key0 < any_sees) {
             const uint8_t* frag = smem + buf * BUF + lane * 16;
             const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + half);

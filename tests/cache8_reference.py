@@ -140,7 +140,9 @@ class Cache:
 
     def attend(self, q, table, lens, scale, mask, q_lens=None, untouched=None):
         """(O, bound): the answer, and how far a bf16 kernel may be off: half a step of the result, half a step of every probability, and what
-        fp32 products and sums of the logits are off by."""
+        fp32 products and sums of the logits are off by.  A probability times its value's scale that lies below the smallest normal number, 2^-126, may count
+        as 0: a key then lacks up to 2^-126 times its code, at most 448 or 127, over a sum of probabilities that is at least 1, the largest one's."""
+        lost = LARGEST[self.fmt] * 2.0 ** -126
         B, H, Nq, d = q.shape
         G = H // self.heads
         cap = table.shape[1] * self.T
@@ -150,22 +152,24 @@ class Cache:
             n = min(max(int(lens[b]), 0), cap)
             rows = Nq if q_lens is None else min(max(int(q_lens[b]), 0), Nq)
             (k, there), (v, _) = self.values("k", table[b], n), self.values("v", table[b], n)
-            for i in range(rows):
-                seen = there & (np.arange(n) <= i + n - rows) if mask else there
-                out[b, :, i] = 0.0
-                if not seen.any():
-                    continue
-                for h in range(H):
-                    kk, vv = k[h // G][seen], v[h // G][seen]
-                    row = q[b, h, i].astype(np.float64)
-                    x = kk @ row * scale
-                    p = np.exp(x - x.max())
-                    p /= p.sum()
-                    o = p @ vv
-                    size = (np.abs(kk) @ np.abs(row)).max() * scale
-                    off = 2.0 ** -8 + 2 * size * (d + 8) * 2.0 ** -24 + len(x) * 2.0 ** -24 + 2.0 ** -20
-                    out[b, h, i] = o
-                    bound[b, h, i] = 2.0 ** -8 * np.abs(o) + off * 1.01 * (p @ np.abs(vv)) + 1e-37
+            out[b, :, :rows] = 0.0
+            k, v = k[:, there], v[:, there]            # what is not there may be anything
+            j = np.arange(n)[there]
+            if not len(j):
+                continue
+            seen = np.ones((rows, len(j)), bool) if not mask else j[None] <= np.arange(rows)[:, None] + n - rows
+            for h in range(H):
+                kk, vv, row = k[h // G], v[h // G], q[b, h, :rows].astype(np.float64)
+                with np.errstate(invalid="ignore"):
+                    x = np.where(seen, row @ kk.T * scale, -np.inf)
+                top = x.max(1, keepdims=True)
+                p = np.exp(x - np.where(np.isinf(top), 0.0, top))
+                total = p.sum(1, keepdims=True)
+                p /= np.where(total > 0, total, 1.0)
+                size = np.where(seen, np.abs(row) @ np.abs(kk).T, 0.0).max(1, keepdims=True) * scale
+                off = 2.0 ** -8 + 2 * size * (d + 8) * 2.0 ** -24 + seen.sum(1, keepdims=True) * 2.0 ** -24 + 2.0 ** -20
+                out[b, h, :rows] = p @ vv
+                bound[b, h, :rows] = 2.0 ** -8 * np.abs(out[b, h, :rows]) + off * 1.01 * (p @ np.abs(vv)) + len(j) * lost
         return out, bound
 
 

@@ -187,7 +187,7 @@ def test_attention_matches_the_definition(lens, H, heads, Nq, T, q_lens, d, fmt,
 @pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("fmt", [E4M3, INT8])
 @pytest.mark.parametrize("lens,H,heads,Nq,T", [([20000], 4, 2, 1, 64), ([9000, 1, 0, 3000, 700], 8, 2, 1, 16), ([5000, 4100], 6, 1, 40, 256), ([12000], 1, 1, 3, 16),
-                                               ([2500, 90, 2000], 2, 2, 300, 64)])
+                                               ([2500, 90, 2000], 2, 2, 300, 64), ([9000, 4000, 100, 0, 7000, 2500], 32, 16, 1, 32), ([6000, 5000, 17], 64, 16, 7, 64)])
 def test_attention_over_keys_divided_over_workgroups(lens, H, heads, Nq, T, d, fmt):
     """Long entries next to short ones and empty ones: parts of several workgroups are put together, and the same call gives the same bits
     whatever the workspace held."""
@@ -203,6 +203,62 @@ def test_attention_over_keys_divided_over_workgroups(lens, H, heads, Nq, T, d, f
         o = attend(dc, q, table, lens, scale, mask)
         check(o, want, bound)
         assert torch.equal(o.view(torch.int16), attend(dc, q, table, lens, scale, mask, poison=False).view(torch.int16))
+
+
+MANY_ROWS = [  # B, H, heads, Nq, longest, T: at least 512 blocks of 128 rows, which a kernel of their own takes
+    (2, 256, 256, 33, 130, 16),
+    (4, 128, 128, 40, 70, 32),          # longer than some entries: queries that see no key
+    (3, 192, 64, 90, 260, 64),          # three query heads to a head of the cache: 270 rows in three blocks
+    (2, 320, 64, 110, 1300, 48),        # more tiles than the blocks of one look-ahead
+    (1, 128, 32, 510, 2300, 256),
+]
+
+
+@pytest.mark.parametrize("B,H,heads,Nq,longest,T", MANY_ROWS)
+@pytest.mark.parametrize("d,fmt,mask", [(32, E4M3, 1), (64, E4M3, 0), (64, INT8, 1), (96, INT8, 1), (128, E4M3, 1), (128, INT8, 0), (256, E4M3, 1)])
+def test_attention_of_many_rows(B, H, heads, Nq, longest, T, d, fmt, mask):
+    """Ragged lengths and query counts, holes, keys whose logits grow along the sequence so that the reference maximum rises in later tiles, and a
+    block that is no number near the end of the last entry."""
+    rng = np.random.default_rng(Nq + d)
+    lens = [longest] + [int(rng.integers(0, longest)) for _ in range(B - 1)]
+    q_lens = [Nq] + [int(rng.integers(0, Nq + 1)) for _ in range(B - 1)]
+    c, table = filled(rng, lens, heads, d, T, fmt)
+    for blk in range(-(-longest // 16)):
+        c.scale["k"][table[0, blk * 16 // T], :, blk % (T // 16)] *= np.float32(2.0 ** min(blk / 16, 4))
+    if longest > 1000:
+        table[0, 3], table[0, 9] = -1, c.n_pages + 2
+    q = ref.bf16(rng.standard_normal((B, H, Nq, d)))
+    scale = float(np.float32(d ** -0.5))
+    print(f"case attend many rows B={B} H={H}/{heads} Nq={Nq} lens={lens} q_lens={q_lens} T={T} d={d} fmt={fmt} mask={mask}", flush=True)
+    want, bound = c.attend(q, table, lens, scale, mask, q_lens, untouched=np.full(q.shape, 7.0))
+    dc = c.device()
+    out = b16(np.full(q.shape, 7.0, np.float32))
+    check(attend(dc, q, table, lens, scale, mask, q_lens, out=out), want, bound)
+    if mask and longest > 200:
+        at = (longest - 17) // 16                       # a whole block that the last positions see, and the first do not
+        dc.v_scale[int(table[0, at * 16 // T]), heads - 1, at % (T // 16)] = float("nan")
+        o = attend(dc, q, table, lens, scale, mask, q_lens).float().cpu().numpy()
+        first = 16 * at - (longest - Nq)                # the first query that sees a token of it
+        hit = o[0, -(H // heads):]
+        assert np.isnan(hit[:, max(first, 0):]).all() and np.isfinite(hit[:, :max(first, 0)]).all() and np.isfinite(o[0, : H - H // heads]).all()
+
+
+@pytest.mark.parametrize("fmt", [E4M3, INT8])
+def test_attention_over_a_few_long_entries_among_many_short_ones(fmt):
+    """More entries than a wavefront has lanes, divided by lengths that only the device knows; and a table with room for far more than the entries have."""
+    rng = np.random.default_rng(15)
+    lens = rng.integers(0, 200, 100)
+    lens[[3, 64, 65, 99]] = [12000, 9001, 30, 11111]
+    q = ref.bf16(rng.standard_normal((100, 3, 1, 64)))
+    c, table = filled(rng, lens, 1, 64, 32, fmt)
+    want, bound = c.attend(q, table, lens, 0.125, 1)
+    check(attend(c.device(), q, table, lens, 0.125, 1), want, bound)
+    few = [5, 0, 40]
+    c, table = filled(rng, few, 2, 128, 16, fmt, extra=3000)
+    q = ref.bf16(rng.standard_normal((3, 4, 2, 128)))
+    assert fa.flat_attn_fwd_cache8_workspace_bytes(3, 4, 2, 2, table.shape[1] * 16, 128) > 0
+    want, bound = c.attend(q, table, few, 0.09, 1)
+    check(attend(c.device(), q, table, few, 0.09, 1), want, bound)
 
 
 def test_attention_over_many_short_entries_and_lengths_out_of_range():
