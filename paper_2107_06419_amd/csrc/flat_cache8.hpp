@@ -53,7 +53,7 @@ hipError_t launch_cache8_compact(const flat_cache8& c, const int* page_table, in
 // Attention over the cache (flat_cache8_fwd.hip).  A row block is rows_per_block of the Nq * (H / heads) rows that share a head of the cache;
 // an entry is a row block of a batch entry, and its keys are divided over one or more units, a workgroup per unit and head.
 struct Cache8Plan {
-    int rows_per_block;  // 16, 32: the wavefronts of a workgroup share the keys of a block's rows; 128: each of four has 32 rows of its own
+    int rows_per_block;  // 16, 32: the wavefronts of a workgroup share the keys of a block's rows; 256 (d = 256: 128): each has 32 rows of its own
     int row_blocks;      // per batch entry, for Nq queries
     int entries;         // B * row_blocks
     int tile_keys;       // what a kernel takes of the keys at a time: a power of two

@@ -11,12 +11,13 @@ namespace flat {
 
 namespace {
 
-// Where a row of a unit's result goes: O if the unit is its entry's only one, else the workspace.
+// Where a row of a batch entry and head of the cache lies in Q and O: row = position * group + query head of the group.
 template <int D>
-__device__ __forceinline__ bf16* row_of_o(const Cache8Args& a, const CacheEntry& t, int kvh, int row) {
+__device__ __forceinline__ size_t row_at(const Cache8Args& a, int b, int kvh, int row) {
     const int pos = a.by_group.quotient(row), g = row - pos * a.group;
-    return a.O + ((size_t)(t.b * (size_t)a.H + kvh * a.group + g) * a.Nq + pos) * D;
+    return ((size_t)(b * (size_t)a.H + kvh * a.group + g) * a.Nq + pos) * D;
 }
+// Partial results of a unit: rows_per_block rows of D, then their reference maxima, then their sums.
 template <int D, int ROWS>
 __device__ __forceinline__ float* part_of(const Cache8Args& a, int u, int kvh) {
     return a.parts + (size_t)(u * (size_t)a.heads + kvh) * (ROWS * (D + 2));
@@ -35,7 +36,7 @@ __device__ __forceinline__ floatx2 four_bf16(const floatx4& y, float by) {
 // A tile is 64 / ROWS blocks: 32 keys on the 32 x 32 x 16 MFMA, 64 keys on the 16 x 16 x 32 one, four products of 16 keys each.  With 16 rows the tokens of
 // K's operand are dealt out likewise, row m of product t is block m / 4, token 4 t + m % 4, and a lane again ends up with the 16 tokens of one block.  The lanes'
 // work per key is half that of 32 rows: 16 workgroups over 4096 keys, 32 rows -> 16, d = 64 18.9 -> 14.8 us, d = 128 26.8 -> 20.1.
-constexpr int NW = 4;  // wavefronts of a workgroup, in both kernels
+constexpr int NW = 4;  // wavefronts of a workgroup, here and in the kernel of many rows at d = 256
 
 // DIVIDED: the entries' keys are divided over units; else a unit is an entry, and its page ids are fetched along with its lengths.
 template <int D, int ROWS, int FMT, bool DIVIDED>
@@ -82,7 +83,6 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
     };
     if (DIVIDED && n_mine) page0 = page_of(0);
 
-    // the rows: row = position * group + query head of the group
     const int row = t.row0 + col, pos = a.by_group.quotient(row);
     const bool has_row = row < t.rows;
     bf16x8 q[2 * NQ];
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             q[2 * j + i] = bf16x8{};
-            if (has_row) q[2 * j + i] = *(const bf16x8*)(row_of_o<D>(a, t, kvh, row) - a.O + a.Q + 16 * (LG * j + grp) + 8 * i);
+            if (has_row) q[2 * j + i] = *(const bf16x8*)(a.Q + row_at<D>(a, t.b, kvh, row) + 16 * (LG * j + grp) + 8 * i);
         }
     }
     const int seen = !has_row ? t.len : a.causal ? min(max(pos + 1 + t.len - t.q_len, 0), t.len) : t.len;  // keys that this row sees
@@ -300,7 +300,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
         }
         float m, l;
         joined(r, &m, &l);
-        *(floatx2*)(row_of_o<D>(a, t, kvh, t.row0 + r) + 4 * c4) = four_bf16(y, l == 0.f ? 0.f : 1.0f / l);
+        *(floatx2*)(a.O + row_at<D>(a, t.b, kvh, t.row0 + r) + 4 * c4) = four_bf16(y, l == 0.f ? 0.f : 1.0f / l);
     }
     if (DIVIDED && unit.n > 1 && tid < rows) {
         part[ROWS * D + tid] = top;
@@ -309,18 +309,247 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
     if (DIVIDED && u == unit.before && kvh == 0 && tid == 0) a.units[unit.e] = make_int2(unit.before, unit.n);
 }
 
-// ---- Many rows: every wavefront has 32 rows of its own and takes all keys of the entry.  The workgroup widens each tile of 64 keys once, in
-// LDS, as the MFMA operands in the order of their lanes (1 KiB each), so that reading and writing them meets no bank twice; while a tile is
-// worked on, the next one's codes are widened and the loads of the one after it are in flight.  One barrier per tile.
+// ---- Many rows: every wavefront has 32 rows of its own and takes all keys of the entry; d up to 128.  The eight wavefronts of a workgroup, two per SIMD, widen
+// each tile of 64 keys once, in LDS, as the MFMA operands in the order of their lanes (1 KiB each), so that reading and writing them meets no bank twice.
+//
+// A step multiplies the last tile's V by its probabilities and this tile's K by Q, 4 D / 16 MFMAs in a row; while they run, the wavefront widens its share of the tile
+// after the next one and asks for its share of the one behind that.  Then come the probabilities.  There are four tiles in LDS: the last one, this one, the next,
+// whose first operands may be asked for, and the one being written; so one barrier per step is enough, and a wavefront's products run beside the vector work of the
+// other one of its SIMD.  What bounds it is power: at d = 128 the clock falls to 1.83 GHz of 2.4 (a large matrix product of the library reaches 53 % of the peak too).
+//
+// The row's largest logit is not looked for in every tile: the probabilities are taken against the reference there is, and their sum, which is needed anyway, shows whether
+// one of them may be above 2^8.  Only then the tile is taken again, with the maximum.  2 x 2048 queries of 16 heads over 16384 keys, d = 128: 566 us with the maximum, a
+// barrier and two tiles in LDS, workgroups of 128 rows; 512 so; two groups of wavefronts in opposite phases 505, d = 64 348 against 319.
 template <int D, int FMT>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(const Cache8Args a, int blocks_per_xcd) {
+__global__ __launch_bounds__(512, 2) void cache8_rows_kernel(const Cache8Args a, int blocks_per_xcd) {
+    constexpr int RW = 8;                               // wavefronts
     constexpr int J = D / 32, PAIRS = 4 * J;            // pairs of operands of a tile: K of (sub-tile, j), then V
-    constexpr int MINE = (PAIRS + NW - 1) / NW;         // of a wavefront: pairs w, w + NW, ...
+    constexpr int MINE = (PAIRS + RW - 1) / RW;         // of a wavefront: pairs w, w + RW
+    constexpr int BUF = PAIRS * 2 * 1024, SLOTS = 4;    // bytes of a tile; tiles in LDS
+    constexpr int GROUP = 16;                           // tiles whose blocks 64 lanes know
+    constexpr int AHEAD = D == 128 ? 3 : 4;             // operands asked for ahead of their MFMA: d = 128 507 us (3) against 533 (4), d = 64 340 against 327
+    extern __shared__ __align__(16) uint8_t smem[];
+    float* scales = (float*)(smem + SLOTS * BUF);       // [2][64 blocks][4]: ks, vs_log2, vs_inv, tokens there as int (-1: a hole)
+    int* numbers = (int*)(scales + 2 * 64 * 4);         // [2][64 blocks]: their numbers in the pool; holes read block 0, and what they read counts for nothing
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5, col = lane & 31;
+    // blocks of one batch entry and head follow each other on one XCD: they read the same codes.  Later rows see more keys: they go first
+    const int id = xcd_logical_block(blockIdx.x, blocks_per_xcd), bh = a.by_row_blocks.quotient(id), b = a.by_heads.quotient(bh), kvh = bh - b * a.heads;
+    if (b >= a.B) return;
+    const CacheEntry t = cache_entry(a, b * a.row_blocks + a.row_blocks - 1 - (id - bh * a.row_blocks));
+    if (t.row0 >= t.rows) return;
+    const int n = t.tiles;
+
+    const int* table = a.page_table + (size_t)t.b * a.max_pages;
+    auto page_of = [&](int group) __attribute__((always_inline)) {
+        const int blk = 4 * GROUP * group + lane;
+        return kCacheBlock * blk < t.len ? table[a.by_page_blocks.quotient(blk)] : -1;
+    };
+    // tells the workgroup of a group's blocks; the result: those of which a token or more is not there
+    auto blocks_of = [&](int group, int page) __attribute__((always_inline)) {
+        const CacheBlock x = cache_block(a, kvh, t.len, 4 * GROUP * group + lane, page);
+        if (w == 0) {
+            *(floatx4*)(scales + 4 * (64 * (group & 1) + lane)) = floatx4{x.ks, x.vs_log2, x.vs_inv, __builtin_bit_cast(float, x.e < 0 ? -1 : x.there)};
+            numbers[64 * (group & 1) + lane] = max(x.e, 0);
+        }
+        return __ballot(x.there < 16);
+    };
+    uint64_t lacking = blocks_of(0, page_of(0)), lacking_next = 0;  // of the group that is worked on, and of the next one
+    int next_page = -1;
+
+    const int row = t.row0 + 32 * w + col;
+    const bool has_row = row < t.rows;
+    bf16x8 q[2 * J];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            q[2 * j + i] = bf16x8{};
+            if (has_row) q[2 * j + i] = *(const bf16x8*)(a.Q + row_at<D>(a, t.b, kvh, row) + 32 * j + 16 * half + 8 * i);
+        }
+    auto seen_by = [&](int r) __attribute__((always_inline)) { return a.causal ? min(max(a.by_group.quotient(r) + 1 + t.len - t.q_len, 0), t.len) : t.len; };
+    const int seen = has_row ? seen_by(row) : t.len;
+    const int all_see = __builtin_amdgcn_readfirstlane(seen_by(t.row0 + 32 * w));  // keys that every row of this wavefront sees
+
+    // this wavefront's operand pairs: p = w, w + RW of [K, V][sub-tile][j]; of each the lane's place in a block, and its block of the tile
+    const uint8_t* base[MINE];
+    int block[MINE];
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) {
+        const int p = min(w + RW * x, PAIRS - 1), is_v = p >= 2 * J, q2 = p - (is_v ? 2 * J : 0), sub = q2 / J;
+        block[x] = 2 * sub + (is_v ? half : (col >> 2) & 1);
+        base[x] = (is_v ? a.v + col * 16 : a.k + (4 * (col >> 3) + (col & 3)) * 16 + half * 256) + 512 * (q2 - sub * J);
+    }
+    uint4v codes[MINE];
+    uint32_t number[MINE];
+    auto in_two_groups = [](int i) __attribute__((always_inline)) { return 4 * (i & (2 * GROUP - 1)); };  // first block of tile i
+    auto find = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+        for (int x = 0; x < MINE; ++x) number[x] = numbers[in_two_groups(i) + block[x]];
+    };
+    auto load = [&](int x) __attribute__((always_inline)) { codes[x] = *(const uint4v*)(base[x] + (uint64_t)number[x] * (16 * D)); };
+    auto clear = [&](int i) __attribute__((always_inline)) {  // what lies behind the entry's last token, of V
+#pragma unroll
+        for (int x = 0; x < MINE; ++x)
+            if (w + RW * x >= 2 * J) codes[x] = clear_behind(codes[x], __builtin_bit_cast(int, scales[4 * (in_two_groups(i) + block[x]) + 3]));
+    };
+    auto widen = [&](int i, int x, int part) __attribute__((always_inline)) {
+        const int p = w + RW * x;
+        if (PAIRS % RW && p >= PAIRS) return;
+        *(bf16x8*)(smem + (i % SLOTS) * BUF + p * 2048 + part * 1024 + lane * 16) = codes_to_bf16<FMT>(codes[x][2 * part], codes[x][2 * part + 1]);
+    };
+
+    floatx16 o[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[j][r] = 0.f;
+    RowState st{-INFINITY, 0.f, 0.f};
+    auto raise = [&](float top) __attribute__((always_inline)) {
+        const float up = __builtin_fmaxf(st.m, top), to = up == -INFINITY ? 0.f : up;
+        const float by = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.sub - to);
+        st.l *= by;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[j][r] *= by;
+        st.m = up;
+        st.sub = to;
+    };
+
+    // the first two tiles; the third is asked for, and the fourth known.  V of the slot before the first meets probabilities of 0: it has to be numbers
+    for (int x = tid; x < BUF / 2 / 16; x += 64 * RW) *(uint4v*)(smem + (SLOTS - 1) * BUF + BUF / 2 + 16 * x) = uint4v{0, 0, 0, 0};
+    __syncthreads();
+    if (n > 0) {
+        for (int i = 0; i < 3; ++i) {
+            find(min(i, n - 1));
+#pragma unroll
+            for (int x = 0; x < MINE; ++x) load(x);
+            if (i == 2) break;
+            clear(min(i, n - 1));
+#pragma unroll
+            for (int x = 0; x < 2 * MINE; ++x) widen(i, x / 2, x % 2);
+        }
+        find(min(3, n - 1));
+    }
+    __syncthreads();
+
+    // What the next group's blocks are: pages at the start of a group, the rest in its middle.  Tiles behind the last one stand for the last, or for whatever their slot
+    // holds: nobody reads them.
+    auto look_ahead = [&](int i) __attribute__((always_inline)) {
+        const int at = i % GROUP;
+        if (at == 0 && i + GROUP < n) next_page = page_of(i / GROUP + 1);
+        if (at == GROUP / 2 && i + GROUP - GROUP / 2 < n) lacking_next = blocks_of(i / GROUP + 1, next_page);
+    };
+    auto done = [&](int i) __attribute__((always_inline)) {
+        if (i % GROUP == GROUP - 1) lacking = lacking_next;
+        look_ahead(i + 1);
+    };
+    auto lacks_after_next = [&](int i) __attribute__((always_inline)) {
+        const int at = i % GROUP + 2;
+        return ((at < GROUP ? lacking >> (4 * at) : lacking_next >> (4 * (at - GROUP))) & 15) != 0;
+    };
+    bf16x8 f[AHEAD];
+    // operand x of step i: V of tile i - 1, then K of tile i
+    auto fetch = [&](int i, int x) __attribute__((always_inline)) {
+        const int k = x - 4 * J;
+        const int at = x < 4 * J ? (2 + x / (2 * J)) * J * 2 + 2 * (x % J) + x / J % 2 : (k & 1) * 2 * J + k / 2;
+        if (x < 8 * J) f[x % AHEAD] = *(const bf16x8*)(smem + ((x < 4 * J ? i + SLOTS - 1 : i) % SLOTS) * BUF + at * 1024 + lane * 16);
+        __builtin_amdgcn_sched_barrier(0x616);  // MFMAs and LDS reads stay in this order: the compiler would ask for an operand just before its use
+    };
+    bf16x8 p[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p[x] = bf16x8{};
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) fetch(0, x);
+    if (n > 0) look_ahead(0);
+    for (int i = 0; i < n;) {
+        floatx16 s[2];
+        floatx4 c[2];
+        for (;;) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[x][r] = 0.f;
+            if (lacks_after_next(i)) clear(i + 2);
+            constexpr int STEP = (8 * J - 2) / (2 * MINE);
+#pragma unroll
+            for (int x = 0; x < 8 * J; ++x) {
+                if (x < 4 * J) o[x % J] = mfma_bf16_32x32x16(f[x % AHEAD], p[x / J], o[x % J]);
+                else s[x & 1] = mfma_bf16_32x32x16(f[x % AHEAD], q[(x - 4 * J) / 2], s[x & 1]);
+                fetch(i, x + AHEAD);
+                if (x % STEP == 1 && x / STEP < 2 * MINE) {
+                    widen(i + 2, x / STEP / 2, x / STEP % 2);
+                    if (x / STEP % 2) load(x / STEP / 2);
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < 2; ++x) c[x] = *(const floatx4*)(scales + 4 * (in_two_groups(i) + 2 * x + half));
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int x = 0; x < AHEAD; ++x) fetch(i + 1, x);
+            find(min(i + 4, n - 1));
+            // a tile that a row does not see whole, or that is not all there, and a reference that has to rise are the other path's: with the rescaling in here, the
+            // compiler moves the accumulators to other registers and back in every tile
+            if (64 * i + 64 > all_see || ((lacking >> (4 * (i % GROUP))) & 15) != 0) break;
+            bf16x8 y[4];
+            float sum[2] = {0.f, 0.f};
+#pragma unroll
+            for (int x = 0; x < 2; ++x) tile_probabilities<false>(s[x], c[x][0], c[x][1], c[x][2], st.sub, 16, &y[2 * x], &y[2 * x + 1], &sum[x]);
+            if (__any(__builtin_fmaxf(sum[0], sum[1]) > (float)(1 << kRescaleAbove) || st.m == -INFINITY)) break;
+            st.l += sum[0] + sum[1];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) p[x] = y[x];
+            done(i);
+            ++i;
+            __builtin_amdgcn_sched_barrier(0);
+            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            if (i >= n) break;
+        }
+        if (i >= n) break;
+        int visible[2];
+        float top = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float last = c[x][3];  // (the bits of a vector's element taken directly would be those of its first)
+            visible[x] = __builtin_bit_cast(int, last) < 0 ? 0 : min(max(seen - 64 * i - 32 * x - kCacheBlock * half, 0), 16);
+            float m = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) m = __builtin_fmaxf(m, r < visible[x] ? s[x][r] : -INFINITY);
+            top = __builtin_fmaxf(top, m == -INFINITY ? m : m * c[x][0]);
+        }
+        top = halves_max(top);
+        if (__any(top > st.m + (kRescaleAbove - 4))) raise(top);  // sixteen probabilities up to 2^4 are no more than 2^8: such logits do not come here again
+#pragma unroll
+        for (int x = 0; x < 2; ++x) tile_probabilities<true>(s[x], c[x][0], c[x][1], c[x][2], st.sub, visible[x], &p[2 * x], &p[2 * x + 1], &st.l);
+        done(i);
+        ++i;
+        __syncthreads();
+    }
+#pragma unroll
+    for (int x = 0; x < 4 * J; ++x) {  // V of the last tile
+        o[x % J] = mfma_bf16_32x32x16(f[x % AHEAD], p[x / J], o[x % J]);
+        if (x + AHEAD < 4 * J) fetch(n, x + AHEAD);
+    }
+    st.l = halves_sum(st.l);
+    if (!has_row) return;
+    const float by = st.l == 0.f ? 0.f : 1.0f / st.l;
+    bf16* to = a.O + row_at<D>(a, t.b, kvh, row) + 4 * half;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) *(floatx2*)(to + 32 * j + 8 * x) = four_bf16(floatx4{o[j][4 * x], o[j][4 * x + 1], o[j][4 * x + 2], o[j][4 * x + 3]}, by);
+}
+
+// ---- Many rows at d = 256: a wavefront's 32 rows take more than 256 registers, so four of them share a tile of 64 keys and one is on each SIMD.  Of two tiles in LDS
+// one is worked on while the next one's codes are widened into the other, and the loads of the one after it are in flight.  One barrier per tile.
+template <int FMT>
+__global__ __launch_bounds__(64 * NW, 1) void cache8_wide_rows_kernel(const Cache8Args a, int blocks_per_xcd) {
+    constexpr int D = 256, J = D / 32, PAIRS = 4 * J;            // pairs of operands of a tile: K of (sub-tile, j), then V
+    constexpr int MINE = PAIRS / NW;                    // of a wavefront: pairs w, w + NW, ...
     constexpr int BUF = PAIRS * 2 * 1024;               // bytes of a tile
     constexpr int GROUP = 16;                           // tiles whose blocks 64 lanes know
-    // The next tile's widening beside Q K^T, or beside P V: 2 x 2048 queries over 16384 keys, d = 64, 345 us against 362, d = 256 (1024 over 8192) 314 / 325, 8 x 512
-    // over 4096, d = 96, 135 / 138; d = 128 566 / 552.  (Hints to the compiler how to mix MFMAs, vector work and LDS reads: 0 to 5 % slower at d = 128.)
-    constexpr bool kWidenFirst = D != 128;
     extern __shared__ __align__(16) uint8_t smem[];
     float* scales = (float*)(smem + 2 * BUF);           // [2][64 blocks][4]: ks, vs_log2, vs_inv, tokens there as int (-1: a hole)
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -353,7 +582,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             q[2 * j + i] = bf16x8{};
-            if (has_row) q[2 * j + i] = *(const bf16x8*)(row_of_o<D>(a, t, kvh, row) - a.O + a.Q + 32 * j + 16 * half + 8 * i);
+            if (has_row) q[2 * j + i] = *(const bf16x8*)(a.Q + row_at<D>(a, t.b, kvh, row) + 32 * j + 16 * half + 8 * i);
         }
     auto seen_by = [&](int r) __attribute__((always_inline)) { return a.causal ? min(max(a.by_group.quotient(r) + 1 + t.len - t.q_len, 0), t.len) : t.len; };
     const int seen = has_row ? seen_by(row) : t.len;
@@ -367,7 +596,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     bool second[MINE];
 #pragma unroll
     for (int x = 0; x < MINE; ++x) {
-        const int p = min(w + NW * x, PAIRS - 1), is_v = p >= 2 * J, q2 = p - (is_v ? 2 * J : 0);
+        const int p = w + NW * x, is_v = p >= 2 * J, q2 = p - (is_v ? 2 * J : 0);
         sub[x] = q2 / J;
         second[x] = is_v ? half : (col >> 2) & 1;
         base[x] = (is_v ? a.v + col * 16 : a.k + (4 * (col >> 3) + (col & 3)) * 16 + half * 256) + 512 * (q2 - sub[x] * J);
@@ -377,7 +606,6 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     auto load = [&](int i) __attribute__((always_inline)) {  // the share of tile i of the unit; `now` is the group it lies in
 #pragma unroll
         for (int x = 0; x < MINE; ++x) {
-            if (PAIRS % NW && w + NW * x >= PAIRS) continue;
             const int at = 4 * (i % GROUP) + 2 * sub[x];
             const int e0 = __builtin_amdgcn_readlane(now_at, at), e1 = __builtin_amdgcn_readlane(now_at, at + 1);
             codes[x] = *(const uint4v*)(base[x] + (uint64_t)(uint32_t)(second[x] ? e1 : e0) * (16 * D));
@@ -387,7 +615,6 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
 #pragma unroll
         for (int x = 0; x < MINE; ++x) {
             const int p = w + NW * x;
-            if (PAIRS % NW && p >= PAIRS) continue;
             uint4v c = codes[x];
             if (!whole && p >= 2 * J) c = clear_behind(c, __builtin_bit_cast(int, scales[4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + 2 * sub[x] + half) + 3]));
             uint8_t* to = smem + buf * BUF + p * 2048 + lane * 16;
@@ -467,11 +694,9 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
             const float* sc = scales + 4 * (64 * ((i / GROUP) & 1) + 4 * (i % GROUP) + half);
             const floatx4 x0 = *(const floatx4*)sc, x1 = *(const floatx4*)(sc + 8);
             floatx16 s[2];
-            if (kWidenFirst) {
-                widen(i + 1, buf ^ 1, true);
-                load(i + 2);
-                ahead = true;
-            }
+            widen(i + 1, buf ^ 1, true);
+            load(i + 2);
+            ahead = true;
             logits(frag, s);
             float top[2];
 #pragma unroll
@@ -488,10 +713,6 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
             tile_probabilities<false>(s[0], x0[0], x0[1], x0[2], st.sub, 16, &p[0], &p[1], &st.l);
             attend(frag, 0, p);
             tile_probabilities<false>(s[1], x1[0], x1[1], x1[2], st.sub, 16, &p[0], &p[1], &st.l);
-            if (!kWidenFirst) {
-                widen(i + 1, buf ^ 1, true);
-                load(i + 2);
-            }
             attend(frag, 1, p);
             ahead = false;
             done(i);
@@ -537,7 +758,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_rows_kernel(
     st.l = halves_sum(st.l);
     if (!has_row) return;
     const float by = st.l == 0.f ? 0.f : 1.0f / st.l;
-    bf16* to = row_of_o<D>(a, t, kvh, row) + 4 * half;
+    bf16* to = a.O + row_at<D>(a, t.b, kvh, row) + 4 * half;
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -603,7 +824,7 @@ __global__ __launch_bounds__(256) void cache8_merge_kernel(const Cache8Args a) {
     for (int k = 1; k < LANES; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) all[i] += __shfl(acc[i], min(k * Q4 + c4, 63));
-    if (lane < Q4) *(floatx2*)(row_of_o<D>(a, t, kvh, row) + 4 * c4) = four_bf16(all, L == 0.f ? 0.f : 1.0f / L);
+    if (lane < Q4) *(floatx2*)(a.O + row_at<D>(a, t.b, kvh, row) + 4 * c4) = four_bf16(all, L == 0.f ? 0.f : 1.0f / L);
 }
 
 // Many parts per entry: a workgroup per row and 32 columns.
@@ -676,7 +897,7 @@ __global__ __launch_bounds__(256) void cache8_merge_many_kernel(const Cache8Args
     if (tid >= Q4) return;
     L = (stat[1][0] + stat[1][1]) + (stat[1][2] + stat[1][3]);
     for (int k = 1; k < LANES; ++k) acc += red[k * Q4 + c4];
-    *(floatx2*)(row_of_o<D>(a, t, kvh, row) + COLS * blockIdx.z + 4 * c4) = four_bf16(acc, L == 0.f ? 0.f : 1.0f / L);
+    *(floatx2*)(a.O + row_at<D>(a, t.b, kvh, row) + COLS * blockIdx.z + 4 * c4) = four_bf16(acc, L == 0.f ? 0.f : 1.0f / L);
 }
 
 template <int D, int ROWS, int FMT, bool DIVIDED>
@@ -699,11 +920,16 @@ hipError_t launch_few(const Cache8Args& args, hipStream_t stream) {
 template <int D, int FMT>
 hipError_t launch_rows(const Cache8Args& args, hipStream_t stream) {
     static std::atomic<uint64_t> lds_allowed{0};
-    constexpr int lds = 2 * (D / 32) * 4 * 2048 + 2 * 64 * 16;
-    const hipError_t e = allow_dynamic_lds((const void*)cache8_rows_kernel<D, FMT>, lds, &lds_allowed);
+    constexpr int tile = (D / 32) * 4 * 2048, lds = D == 256 ? 2 * tile + 2 * 64 * 16 : 4 * tile + 2 * 64 * 20;
+    static_assert(lds <= 160 * 1024, "the tiles must fit the LDS");
+    const auto kernel = [] {
+        if constexpr (D == 256) return cache8_wide_rows_kernel<FMT>;
+        else return cache8_rows_kernel<D, FMT>;
+    }();
+    const hipError_t e = allow_dynamic_lds((const void*)kernel, lds, &lds_allowed);
     if (e != hipSuccess) return e;
     const int per_xcd = (int)(((long long)args.entries * args.heads + 7) / 8);
-    hipLaunchKernelGGL((cache8_rows_kernel<D, FMT>), dim3((unsigned)per_xcd * 8u), dim3(64 * NW), lds, stream, args, per_xcd);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)per_xcd * 8u), dim3(D == 256 ? 64 * NW : 512), lds, stream, args, per_xcd);
     return hipGetLastError();
 }
 
@@ -719,7 +945,7 @@ hipError_t launch_merge(const Cache8Args& args, hipStream_t stream) {
 template <int D, int FMT>
 hipError_t launch(const Cache8Args& args, hipStream_t stream) {
     hipError_t e = hipErrorInvalidValue;
-    if (args.rows_per_block == 128) e = launch_rows<D, FMT>(args, stream);
+    if (args.rows_per_block > 32) e = launch_rows<D, FMT>(args, stream);
     else if (args.rows_per_block == 32) e = launch_few<D, 32, FMT>(args, stream);
     else if constexpr (D % 64 == 0) e = launch_few<D, 16, FMT>(args, stream);
     return e != hipSuccess || args.limit == 0 ? e : launch_merge<D>(args, stream);

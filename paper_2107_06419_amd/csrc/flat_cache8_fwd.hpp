@@ -151,10 +151,9 @@ constexpr int kRescaleAbove = 8;  // log2: the reference maximum rises only when
 // bf16, and *sum gets the sum of the block's p.  visible: tokens of the block that the row sees (all if !EDGE).
 template <bool EDGE, typename S>
 __device__ __forceinline__ void tile_probabilities(const S& s, float c, float vs_log2, float vs_inv, float sub, int visible, bf16x8* lo, bf16x8* hi, float* l) {
-    constexpr uint32_t kOnes = 0x3f803f80u;
     const float b = vs_log2 - sub;
     uint4v plo, phi;
-    float sum = 0.f;
+    float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
         float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], c, b)), p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r + 1], c, b));
@@ -163,13 +162,14 @@ __device__ __forceinline__ void tile_probabilities(const S& s, float c, float vs
             p1 = r + 1 < visible ? p1 : 0.f;
         }
         const uint32_t w = pack_bf16(p0, p1);
-        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), __builtin_bit_cast(bf16x2, kOnes), sum, false);
+        sum0 += p0;
+        sum1 += p1;
         if (r < 8) plo[r / 2] = w;
         else phi[r / 2 - 4] = w;
     }
     *lo = __builtin_bit_cast(bf16x8, plo);
     *hi = __builtin_bit_cast(bf16x8, phi);
-    if (!EDGE || visible > 0) *l = __builtin_fmaf(sum, vs_inv, *l);  // a scale that is no number is none of a row that does not see the block
+    if (!EDGE || visible > 0) *l = __builtin_fmaf(sum0 + sum1, vs_inv, *l);  // a scale that is no number is none of a row that does not see the block
 }
 
 // v_mfma_f32_16x16x32_bf16:  D[16x16] += A[16x32] * B[32x16].  A: lane l holds row (l % 16), contraction indices 8 (l / 16) .. + 7; B: column (l % 16), the

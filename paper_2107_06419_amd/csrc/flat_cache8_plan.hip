@@ -8,9 +8,10 @@ namespace flat {
 // Which kernel an attention call takes, and whether the keys of its entries are divided over workgroups.  Figures: e4m3, 4 query heads to a head of the cache,
 // us, a hipGraph of ten calls; BH = batch entries * heads of the cache.
 //
-// Blocks of 16 or 32 rows, whose keys the four wavefronts of a workgroup share, or of 128 rows, whose tiles are widened once for four wavefronts: the latter
-// need 512 workgroups (256 at d = 256, where one fills a compute unit) to be ahead, whatever the number of keys.  BH = 32, 2048 rows, d = 128 (512 blocks): 512 keys 37.3 against 36.6,
-// 2048 97 / 94, 8192 323 / 300; BH = 128, 512 rows, 8192 keys 353 / 317; half as many, BH = 8, 2048 rows, 8192 keys 93 / 113; d = 256, 256 blocks of 2048 keys 128 / 117, 128 blocks 61 / 86.
+// Blocks of 16 or 32 rows, whose keys the four wavefronts of a workgroup share, or of 256 (d = 256: 128), whose tiles are widened once for eight (four) wavefronts of 32 rows.
+// The latter are ahead where there is one for each of the 256 compute units and 7 of 8 of their wavefronts have rows.  256 blocks of 4096 keys, blocks of 32 / 256 rows: d = 128
+// 199 / 155, d = 64 109 / 104; d = 32, 2048 keys 54 / 51; d = 96 78 / 76; d = 256 121 / 107; half as many blocks, d = 128 98 / 131, d = 64 59 / 94, d = 256 66 / 101; a quarter of the
+// wavefronts without rows, d = 128 157 / 155, d = 64 86 / 105, d = 32 42 / 48, d = 96 61 / 73, d = 256 98 / 104.
 //
 // Dividing costs a launch and the parts' way through memory, 5 us and more, and gives shorter walks over the keys and even shares of a ragged batch.  A workgroup takes
 // about 5.5 us and `round` per step of its four wavefronts, but no less than the memory takes for the codes of all of them at 5.2 TB/s, counted at 0.45: a batch is as often
@@ -21,7 +22,10 @@ void cache8_plan(int B, int H, int heads, int Nq, int max_tokens, int d, Cache8P
     constexpr int kLeastKeys = 256;
     const int held = d == 256 ? 256 : 512;  // workgroups that 256 compute units hold at once
     const long long rows = (long long)Nq * (H / heads);
-    out->rows_per_block = rows > 32 && (rows + 127) / 128 * B * heads >= held ? 128 : rows <= 16 && d % 64 == 0 ? 16 : 32;
+    const int many = d == 256 ? 128 : 256;
+    const long long blocks = (rows + many - 1) / many;
+    const bool filled = blocks * B * heads >= 256 && 8 * ((rows + 31) / 32) >= 7 * blocks * (many / 32);
+    out->rows_per_block = filled ? many : rows <= 16 && d % 64 == 0 ? 16 : 32;
     out->row_blocks = (int)((rows + out->rows_per_block - 1) / out->rows_per_block);
     const long long entries = (long long)B * out->row_blocks, grid = entries * heads;
     out->entries = (int)entries;

@@ -243,6 +243,67 @@ def test_attention_of_many_rows(B, H, heads, Nq, longest, T, d, fmt, mask):
         assert np.isnan(hit[:, max(first, 0):]).all() and np.isfinite(hit[:, :max(first, 0)]).all() and np.isfinite(o[0, : H - H // heads]).all()
 
 
+SHARED_TILES = [  # B, H, heads, Nq, longest, T: at least 256 blocks of 256 rows (d = 256: 128), most of whose wavefronts have rows
+    (2, 128, 128, 250, 130, 16),
+    (4, 64, 64, 225, 70, 32),           # longer than some entries: queries that see no key
+    (3, 258, 86, 250, 260, 64),         # three query heads to a head of the cache: 750 rows in three blocks
+    (2, 320, 64, 100, 1300, 48),        # more tiles than the blocks of one look-ahead
+    (8, 32, 32, 256, 16, 16),           # one tile, or none
+    (1, 64, 64, 1000, 2111, 32),
+]
+
+
+@pytest.mark.parametrize("B,H,heads,Nq,longest,T", SHARED_TILES)
+@pytest.mark.parametrize("d,fmt,mask,q_size", [(32, E4M3, 1, 1), (32, INT8, 0, 30), (64, E4M3, 0, 30), (64, INT8, 1, 1), (96, E4M3, 1, 30), (128, E4M3, 1, 1), (128, E4M3, 0, 30), (128, INT8, 1, 3),
+                                               (256, E4M3, 1, 30)])
+def test_attention_of_rows_that_share_tiles(B, H, heads, Nq, longest, T, d, fmt, mask, q_size):
+    """Ragged lengths from 0 on and query counts, holes, logits of some units and of hundreds, which grow along the sequence in steps: the reference maximum
+    rises a little or by more than a float holds; and a block that is no number."""
+    rng = np.random.default_rng(Nq + d + q_size)
+    lens = [longest] + [int(rng.integers(0, longest)) for _ in range(B - 1)]
+    q_lens = [Nq] + [int(rng.integers(0, Nq + 1)) for _ in range(B - 1)]
+    if B > 2:
+        lens[1] = 0
+    c, table = filled(rng, lens, heads, d, T, fmt)
+    for blk in range(-(-longest // 16)):
+        c.scale["k"][table[0, blk * 16 // T], :, blk % (T // 16)] *= np.float32(2.0 ** min(blk // 12, 4))
+    if longest > 1000:
+        table[0, 3], table[0, 9] = -1, c.n_pages + 2
+    q = ref.bf16(rng.standard_normal((B, H, Nq, d)) * q_size)
+    scale = float(np.float32(d ** -0.5))
+    print(f"case attend shared tiles B={B} H={H}/{heads} Nq={Nq} lens={lens} q_lens={q_lens} T={T} d={d} fmt={fmt} mask={mask} q_size={q_size}", flush=True)
+    want, bound = c.attend(q, table, lens, scale, mask, q_lens, untouched=np.full(q.shape, 7.0))
+    dc = c.device()
+    check(attend(dc, q, table, lens, scale, mask, q_lens, out=b16(np.full(q.shape, 7.0, np.float32))), want, bound)
+    if longest > 200:
+        at = (longest - 17) // 16
+        dc.v_scale[int(table[0, at * 16 // T]), heads - 1, at % (T // 16)] = float("nan")
+        o = attend(dc, q, table, lens, scale, mask, q_lens).float().cpu().numpy()
+        first = max(16 * at - (longest - Nq), 0) if mask else 0
+        hit = o[0, -(H // heads):]
+        assert np.isnan(hit[:, first:]).all() and np.isfinite(hit[:, :first]).all() and np.isfinite(o[0, : H - H // heads]).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_logits_that_stay_somewhat_above_the_first_ones(d):
+    """Rows of 256-row blocks whose first keys have logit 0 and whose later ones 2, 3, ... 9 in base 2: around what lets the reference maximum be, and sums of
+    sixteen of them around what does not."""
+    rng = np.random.default_rng(d)
+    B, heads, Nq, n = 4, 64, 256, 640
+    c = ref.Cache(B * n // 64, heads, 64, d, E4M3, rng)
+    table = np.arange(B * n // 64, dtype=np.int32).reshape(B, -1)
+    c.scale["k"][:], c.scale["v"][:] = 1.0, 2.0 ** -6
+    c.codes["k"][:] = 0
+    v = ref.to_codes(rng.standard_normal(c.codes["v"].shape) * 40, E4M3)
+    c.codes["v"][:] = v
+    for t in range(1, n // 64):      # channel 0 alone tells the keys apart: 1, 1.125, 1.25, ...
+        c.codes["k"][t::n // 64, :, :, :, 0] = ref.to_codes(np.full(c.codes["k"][t::n // 64, :, :, :, 0].shape, 1.0 + t / 8), E4M3)
+    q = np.zeros((B, heads, Nq, d))
+    q[..., 0] = ref.bf16(np.log(2.0) * rng.integers(1, 9, (B, heads, Nq)) / 2)
+    want, bound = c.attend(q, table, [n] * B, 2.0, 0)
+    check(attend(c.device(), q, table, [n] * B, 2.0, 0), want, bound)
+
+
 @pytest.mark.parametrize("fmt", [E4M3, INT8])
 def test_attention_over_a_few_long_entries_among_many_short_ones(fmt):
     """More entries than a wavefront has lanes, divided by lengths that only the device knows; and a table with room for far more than the entries have."""
