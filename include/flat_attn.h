@@ -252,7 +252,8 @@ int flat_attn_rope_freqs(double* out, int rot_d, double base, int scaling, doubl
  * FLAT_CACHE8_BLOCK tokens of a head has a scale for its keys and one for its values, and a value is code * scale.
  *   k, v: device, 16-byte aligned, n_pages * n_heads * page_tokens * d codes each.  In memory order, K is [n_pages][n_heads][page_tokens / 16][d / 16]
  *     [16 tokens][16 channels], V [n_pages][n_heads][page_tokens / 16][d][16 tokens].
- *   k_scale, v_scale: device, 4-byte aligned, float [n_pages][n_heads][page_tokens / 16], each >= 0 and finite (or NaN: the block is not a number).
+ *   k_scale, v_scale: device, 4-byte aligned, float [n_pages][n_heads][page_tokens / 16], each >= 0 and finite (or NaN: the block is not a number).  Scales that the
+ *     caller computes are best 0 or between 2^-100 and 2^100: outside, products of a scale and a code or a probability may leave the range of fp32.
  *   page_tokens: a multiple of 16, at most 65536.  d: 32, 64, 96, 128 or 256.
  *   format: FLAT_CACHE8_E4M3 (4 exponent and 3 fraction bits, largest 448, no infinity; NaN codes are not to be stored) or FLAT_CACHE8_INT8 (-127 .. 127).
  *   n_pages * n_heads * page_tokens / 16 is at most 2^31 - 1.
@@ -294,7 +295,7 @@ int flat_attn_cache8_write(const flat_cache8* cache, const void* K, const void* 
  *   mask_kind FLAT_MASK_CAUSAL: an entry's queries are the last q_lens[b] of its lens[b] positions, so query i sees token j iff
  *     j <= i + lens[b] - q_lens[b].  A query that sees no token gives zeros.
  *   workspace: device, 16-byte aligned, at least flat_attn_fwd_cache8_workspace_bytes() bytes (same B, H, n_heads, Nq, d; max_tokens = max_pages *
- *     page_tokens), overwritten; may be NULL where that is 0.  It overlaps no other buffer.
+ *     page_tokens), overwritten; may be NULL where that is 0.  Enough for some page table, it is enough for every narrower one.  It overlaps no other buffer.
  * Logits, softmax statistics and sums in fp32, probabilities (times the value's scale) rounded to bf16, as flat_attn_fwd.  How the keys of an entry are
  * divided over workgroups follows from the lengths of the whole batch, so an entry's last bits may change with its neighbours' lengths; the same call gives the same bits.
  */
