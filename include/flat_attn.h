@@ -256,7 +256,7 @@ int flat_attn_rope_freqs(double* out, int rot_d, double base, int scaling, doubl
  *     caller computes are best 0 or between 2^-100 and 2^100: outside, products of a scale and a code or a probability may leave the range of fp32.
  *   page_tokens: a multiple of 16, at most 65536.  d: 32, 64, 96, 128 or 256.
  *   format: FLAT_CACHE8_E4M3 (4 exponent and 3 fraction bits, largest 448, no infinity; NaN codes are not to be stored) or FLAT_CACHE8_INT8 (-127 .. 127).
- *   n_pages * n_heads * page_tokens / 16 is at most 2^31 - 1.
+ *   n_pages * n_heads * page_tokens / 16 is at most 2^31 - 1, max_pages * page_tokens of a page table at most 2^31 - 65537.
  * The struct is read during a call and not kept.  Checks common to the entry points that take one: FLAT_ERR_NULL, FLAT_ERR_SHAPE (a count not
  * positive, page_tokens no multiple of 16, too many blocks), FLAT_ERR_UNSUPPORTED (d, format), FLAT_ERR_ALIGN, FLAT_ERR_ALIAS (outputs overlap).
  * Lengths, page tables and lists live on the device and are not validated by the host: lengths are clamped to what the page table has room for, ids

@@ -49,9 +49,11 @@ int check_cache(const flat_cache8* c, Span (&buf)[4]) {
     return FLAT_OK;
 }
 
-// A page table of `rows` rows over pages of page_tokens tokens: its token numbers and its entries fit 31 bits.
+// A page table of `rows` rows over pages of page_tokens tokens: its entries fit 31 bits, and so do its token numbers and those some thousands behind its end, which wavefronts
+// that know their blocks in groups look at.
+constexpr long long kMaxTokens = kMaxInt - 65536;
 bool table_fits(int rows, int max_pages, int page_tokens) {
-    return rows > 0 && max_pages > 0 && max_pages <= (kMaxInt - 64) / page_tokens && (long long)rows * max_pages <= kMaxInt;
+    return rows > 0 && max_pages > 0 && max_pages <= kMaxTokens / page_tokens && (long long)rows * max_pages <= kMaxInt;
 }
 
 int from_hip(hipError_t e) { return e == hipSuccess ? FLAT_OK : FLAT_ERR_HIP; }
@@ -102,7 +104,7 @@ int flat_attn_cache8_write(const flat_cache8* cache, const void* K, const void* 
 
 // What the attention call can number; its plan on success.
 static bool attend_plan(int B, int H, int heads, int Nq, long long max_tokens, int d, flat::Cache8Plan* plan) {
-    if (B <= 0 || H <= 0 || heads <= 0 || Nq <= 0 || H % heads || max_tokens <= 0 || max_tokens > kMaxInt - 64 || !head_dim(d)) return false;
+    if (B <= 0 || H <= 0 || heads <= 0 || Nq <= 0 || H % heads || max_tokens <= 0 || max_tokens > kMaxTokens || !head_dim(d)) return false;
     const long long rows = (long long)Nq * (H / heads);
     if (rows > kMaxInt / 2 || (long long)B * heads > kMaxInt / 2 / rows) return false;  // the grids: one workgroup per row in the merge
     if ((unsigned long long)Nq * (unsigned)d * 2u > 0xffffffffULL) return false;

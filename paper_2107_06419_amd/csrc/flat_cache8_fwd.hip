@@ -319,7 +319,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void cache8_few_rows_ker
 //
 // The row's largest logit is not looked for in every tile: the probabilities are taken against the reference there is, and their sum, which is needed anyway, shows whether
 // one of them may be above 2^8.  Only then the tile is taken again, with the maximum.  2 x 2048 queries of 16 heads over 16384 keys, d = 128: 566 us with the maximum, a
-// barrier and two tiles in LDS, workgroups of 128 rows; 512 so; two groups of wavefronts in opposite phases 505, d = 64 348 against 319.
+// barrier and two tiles in LDS, workgroups of 128 rows; 488 so; two groups of wavefronts in opposite phases 505, d = 64 348 against 319.
 template <int D, int FMT>
 __global__ __launch_bounds__(512, 2) void cache8_rows_kernel(const Cache8Args a, int blocks_per_xcd) {
     constexpr int RW = 8;                               // wavefronts

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * kWaves) void cache8_write_kernel(const WriteAr
     int n = a.n_new ? min(max(a.n_new[b], 0), a.N) : a.N;
     n = min(n, a.max_tokens - start);
     const int blk = start / kCacheBlock + j, tok0 = blk * kCacheBlock;
-    if (n <= 0 || tok0 >= start + n) return;
+    if (n <= 0 || blk > (start + n - 1) / kCacheBlock) return;  // (by blocks: the last token numbers that N could reach may lie beyond 2^31)
     const int page = a.page_table[(size_t)b * a.max_pages + a.by_page_blocks.quotient(blk)];
     if ((unsigned)page >= (unsigned)a.n_pages) return;
     const int e = (page * a.heads + head) * a.page_blocks + blk - a.by_page_blocks.quotient(blk) * a.page_blocks;

@@ -189,3 +189,14 @@ def test_validation_code_is_clean_under_asan_and_ubsan():
         run = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
         out = run.stdout + run.stderr
         assert run.returncode == 0 and "cache8 host checks passed" in out and "runtime error" not in out, out[-4000:]
+
+
+def test_page_tables_whose_tokens_pass_31_bits_are_refused():
+    """Token numbers are 31 bits wide, and wavefronts look at blocks up to some thousands of tokens behind an entry's last."""
+    for tokens in (16, 48, 65536):
+        most = (2 ** 31 - 65537) // tokens
+        assert write(max_pages=most + 1, page_tokens=tokens, B=1) == -2 and attend(max_pages=most + 1, page_tokens=tokens, B=1) == -2
+        assert fork(max_pages=most + 1, page_tokens=tokens, n_seqs=1) == -2 and compact(max_pages=most + 1, page_tokens=tokens, n_seqs=1) == -2
+        assert attend(max_pages=most, page_tokens=tokens, B=1, lens=A[7] + 2) == -4 and write(max_pages=most, page_tokens=tokens, B=1, lens=A[7] + 2) == -4
+    size = fa.flat_attn_fwd_cache8_workspace_bytes
+    assert size(1, 1, 1, 1, 2 ** 31 - 65537, 128) == size(1, 1, 1, 1, 1 << 20, 128) > 0 and size(1, 1, 1, 1, 2 ** 31 - 65536, 128) == 0

@@ -399,6 +399,30 @@ def test_pools_beyond_four_gigabytes():
     check(attend(big, q, np.array([[7, n_pages - 70000, n_pages - 2]]), [n], 0.0625, 0), want, bound)
 
 
+def test_token_numbers_near_31_bits():
+    """The widest page table there is, of holes but for its first page and its last two: lengths and token numbers close to 2^31, and a write whose rows would pass it."""
+    import torch
+    T, d, width = 65536, 32, (2 ** 31 - 65537) // 65536
+    rng = np.random.default_rng(31)
+    cap = width * T
+    small = ref.Cache(3, 1, T, d, E4M3)
+    start, N = cap - 37, 131_200                                # the last 37 tokens there is room for, of rows that go on beyond 2^31
+    x, y = (ref.bf16(rng.standard_normal((1, 1, N, d))) for _ in range(2))
+    dc = small.device()
+    table = np.full((1, width), -1, np.int32)
+    table[0, [0, width - 2, width - 1]] = [1, 0, 2]
+    fa.flat_attn_cache8_write(dc, b16(x), b16(y), i32(table), i32([start]))
+    first = [ref.bf16(rng.standard_normal((1, 1, 50, d))) for _ in range(2)]
+    fa.flat_attn_cache8_write(dc, b16(first[0]), b16(first[1]), i32(table), i32([0]))
+    small.write(first[0], first[1], np.array([[1, 0, 2]], np.int32), [0])
+    small.write(x[:, :, :37], y[:, :, :37], np.array([[1, 0, 2]], np.int32), [3 * T - 37])
+    small.like(dc).assert_same(small)
+    q = ref.bf16(rng.standard_normal((1, 2, 3, d)))
+    for n in (cap, cap - 5):                                    # holes count for nothing: a short table with the same tokens
+        want, bound = small.attend(q, np.array([[1, 0, 2]], np.int32), [3 * T - (cap - n)], 2.0, 1)
+        check(attend(dc, q, table, [n], 2.0, 1), want, bound)
+
+
 # ---- pages ---------------------------------------------------------------------------------------------------------------------------------
 
 def random_cache(rng, n_pages=23, heads=3, T=32, d=32):
