@@ -176,6 +176,15 @@ __device__ __forceinline__ void list_kept(const uint64_t* groups, int first, int
     }
 }
 
+__device__ __forceinline__ void fill_unused(int* list, int n) {
+    const int tid = threadIdx.x, head = min((int)((0 - (reinterpret_cast<uintptr_t>(list) >> 2)) & 3), n);
+    const int quads = (n - head) / 4, tail = n - head - 4 * quads;
+    if (tid < head) list[tid] = -1;
+    if (tid < tail) list[head + 4 * quads + tid] = -1;
+    uint4v* body = (uint4v*)(list + head);
+    for (int i = tid; i < quads; i += kListThreads) body[i] = uint4v{~0u, ~0u, ~0u, ~0u};
+}
+
 // Bits of group g that are pages below `end`.
 __device__ __forceinline__ uint64_t below(int g, int end) {
     const int n = end - 64 * g;
@@ -193,6 +202,7 @@ __global__ __launch_bounds__(kListThreads) void cache8_free_kernel(int* page_tab
         for (int x = tid & 63; x < max_pages; x += 64) page_table[(size_t)s * max_pages + x] = -1;
         if ((tid & 63) == 0) lens[s] = 0;
     }
+    fill_unused(unused, n_pages);  // all of it, while the table is on its way; the list overwrites its beginning
     __syncthreads();  // the rows are read below
     mark_held((uint32_t*)bitmap, n_pages, page_table, n_seqs * max_pages);
     const int groups = (n_pages + 63) / 64, share = (groups + kListWaves - 1) / kListWaves;
@@ -201,7 +211,6 @@ __global__ __launch_bounds__(kListThreads) void cache8_free_kernel(int* page_tab
     int before, total;
     count_kept(bitmap, first, last, sums, keep, &before, &total);
     list_kept(bitmap, first, last, keep, unused, before);
-    for (int i = total + tid; i < n_pages; i += kListThreads) unused[i] = -1;
     if (tid == 0) *n_unused = total;
 }
 
