@@ -150,6 +150,7 @@ constexpr int kRescaleAbove = 8;  // log2: the reference maximum rises only when
 // Probabilities of a tile: s holds the logits of the lane's row and block, token by token.  c: the block's key scale; the result is p * vs in
 // bf16, and *l gets the sum of the block's p.  visible: tokens of the block that the row sees (all if !EDGE).  The sum is of the fp32 values, by additions: a bf16 dot product adds two
 // at a time, but waits for the matrix unit; beside another wavefront's MFMAs 32 of them take 1197 cycles (without 161), 32 additions 204 (159).
+// (Summing what the product's rounding left would cost two more instructions a pair; without, the error against 64 bits is 2.2e-3 instead of 2.0e-3, 2-norm.)
 template <bool EDGE, typename S>
 __device__ __forceinline__ void tile_probabilities(const S& s, float c, float vs_log2, float vs_inv, float sub, int visible, bf16x8* lo, bf16x8* hi, float* l) {
     const float b = vs_log2 - sub;
